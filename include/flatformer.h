@@ -245,6 +245,113 @@ int ff_group_attention(const void* feats, void* out, int64_t n,
 #define FF_PATH_FUSED 1
 int ff_group_attention_path(const ff_layer_weights* w, int G, int dtype, uint32_t flags);
 
+/* ---- attention over rows that the caller holds, and its gradient -----------------------------------------
+ * The attention of the layers by itself, for programs with layers of their own: queries, keys and values come in
+ * as rows of heads, groups as the lists that the sorts write (or any other cut of the rows), and what a backward pass
+ * needs goes out beside the result.  Per group and head, over the keys j of the group that the mask leaves:
+ *
+ *   s_ij = scale q_i . k_j     lse_i = log sum_j exp(s_ij)     out_i = sum_j exp(s_ij - lse_i) v_j
+ *
+ * and, for the gradient g_i of out_i, with p_ij = exp(s_ij - lse_i), delta_i = g_i . out_i and
+ * e_ij = p_ij (g_i . v_j - delta_i):
+ *
+ *   dq_i = scale sum_j e_ij k_j     dk_j = scale sum_i e_ij q_i     dv_j = sum_i p_ij g_i
+ *
+ * the last two summed also over the query heads that share a key head.  A query whose group holds no key, or none that the mask
+ * leaves, gets out = 0, lse = -infinity and dq = 0, and a key without queries, or one that the mask takes out, dk = dv = 0.
+ * What a masked row of k or v holds is of no account, infinities and NaNs included.
+ *
+ * ff_heads: element e of head h of row r lies at data[r * row_stride + h * head_stride + e] (strides in elements, none
+ * negative).  Inputs may have strides of zero; rows and heads of an output must not share elements with each other,
+ * with an input or with another output (parts of one packed array may lie beside each other).  Rows whose address, strides and
+ * head_dim are multiples of 16 bytes are read and written in pieces of 16 bytes, others element by element (slower, same results).
+ *
+ * ff_group_list: group g owns positions offsets[g] .. min(offsets[g+1], offsets[g]+G)-1 of 0..n-1, and position p stands for row
+ * perm[p], or for row p where perm is NULL.  Offsets ascend; no row stands at two positions of a list.  offsets holds max_groups + 1
+ * readable entries, of which the first *num_groups + 1 count (num_groups NULL: max_groups + 1); *num_groups < 0 (a failed
+ * sort) computes nothing.  The lists of the sorts fit as they are, with FF_TAIL_DROP too.  queries and keys may be the same list
+ * (attention inside every group) or two (queries over other rows); both have the same groups.  Rows that no group of a
+ * list covers are left as they were in out, lse and the gradients.  Offsets outside 0..n are cut there and positions whose row is
+ * outside 0..n-1 are passed over, so that no list makes a call leave its buffers.
+ *
+ * Results do not depend on timing: the same call gives the same bits.  16-bit types: products of that type with float32 sums;
+ * scores, softmax, lse, delta and all sums are float32, and p and e are rounded to the type where they enter a product.
+ * FF_F32: float32 throughout.
+ * Limits (FF_ERR_UNSUPPORTED otherwise): head_dim 1..128, heads a multiple of kv_heads, rows < 2^31, and at most 2^31 - 1
+ * workgroups a launch (tiles of 16 rows and more, times heads). */
+typedef struct {
+  void* data; /* read only where it is an input */
+  int64_t row_stride, head_stride;
+} ff_heads;
+
+typedef struct {
+  const int32_t* perm;    /* [n], or NULL */
+  const int32_t* offsets; /* [max_groups + 1] */
+  int64_t n;              /* rows */
+  int32_t G;              /* most positions of a group, >= 1 (n: no bound of its own) */
+} ff_group_list;
+
+typedef struct {
+  int32_t heads, kv_heads, head_dim;
+  float scale;                /* finite, usually 1 / sqrt(head_dim) */
+  const int32_t* num_groups;  /* device scalar, or NULL */
+  int32_t max_groups;
+  ff_group_list queries, keys;
+  const uint8_t* key_mask;    /* NULL, or [keys.n]: 0 takes the row out */
+} ff_attention_shape;
+
+/* workspace: ff_attention_workspace_bytes(a, dtype) bytes, 256-byte aligned (0 for most shapes: then it may be NULL).
+ * lse: float32 [queries.n, heads], or NULL where nothing needs it. */
+size_t ff_attention_workspace_bytes(const ff_attention_shape* a, int dtype);
+
+int ff_attention(const ff_attention_shape* a, const ff_heads* q, const ff_heads* k, const ff_heads* v, const ff_heads* out,
+                 float* lse, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* out and lse as ff_attention wrote them for the same a, q, k and v; dout: the gradient of out. */
+size_t ff_attention_backward_workspace_bytes(const ff_attention_shape* a, int dtype);
+
+int ff_attention_backward(const ff_attention_shape* a, const ff_heads* q, const ff_heads* k, const ff_heads* v,
+                          const ff_heads* out, const float* lse, const ff_heads* dout, const ff_heads* dq,
+                          const ff_heads* dk, const ff_heads* dv, int dtype, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* ---- rotary positions of queries and keys ----------------------------------------------------------------
+ * Turns pairs of elements of every head of a row by angles that grow with the row's positions, so that a product of a query with a
+ * key depends on how far apart the two lie.  Position columns (one for a place in a sequence; x and y, or x, y and z, of a pillar
+ * or voxel: coords + 1 with a row stride of 3 or 4) each own 2 * pairs elements of the head, one column after the other:
+ *
+ *   (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t),   t = position[column] * freqs[column][i],   i < pairs
+ *
+ * FF_ROTARY_HALF: a is element i and b element pairs + i of the column's part; FF_ROTARY_INTERLEAVED: a is element 2 i and b
+ * element 2 i + 1.  Elements from 2 * axes * pairs on pass through.  With inverse set the angles are negated: the gradient of
+ * the turned rows goes back to that of the rows.  Angles are float64 before they are reduced to one turn, so far positions keep
+ * their precision; the result is rounded once.
+ * q (q_heads heads of n rows) and k (k_heads, or 0 and k NULL) are turned in one launch; q_out may be q, and k_out may be k
+ * (same address and strides); other overlaps are FF_ERR_ARG.
+ * Limits (FF_ERR_UNSUPPORTED otherwise): axes 1..3, 1 <= axes * pairs <= 128, 2 * axes * pairs <= head_dim <= 256. */
+typedef struct {
+  int32_t axes, pairs; /* position columns, and turned pairs of each */
+  int32_t layout;      /* FF_ROTARY_HALF | FF_ROTARY_INTERLEAVED */
+  int32_t inverse;     /* 0 | 1 */
+  float amplitude;
+  const double* freqs; /* device [axes][pairs], radians a position */
+} ff_rotary_spec;
+#define FF_ROTARY_HALF 0
+#define FF_ROTARY_INTERLEAVED 1
+
+int ff_rotary(const ff_heads* q, const ff_heads* q_out, int32_t q_heads, const ff_heads* k, const ff_heads* k_out,
+              int32_t k_heads, int64_t n, int32_t head_dim,
+              const int32_t* positions /* column c of row r at [r * position_row_stride + c * position_axis_stride] */,
+              int64_t position_row_stride, int64_t position_axis_stride, const ff_rotary_spec* spec, int dtype, void* stream);
+
+/* Frequencies of `pairs` pairs into a HOST array: f_i = base^(-i / pairs), stretched for contexts `factor` times as long as the
+ * original one.  original_length 0: all by the factor, f_i / factor.  Else a pair that makes high_turns turns or more over
+ * original_length positions stays, one that makes low_turns or fewer is divided by the factor, and in between
+ * f_i (w + (1 - w) / factor) with w = (turns - low_turns) / (high_turns - low_turns).
+ * FF_ERR_ARG: NULL, pairs < 1, base or factor not positive and finite, original_length < 0, high_turns <= low_turns. */
+int ff_rotary_frequencies(double* freqs /* host [pairs] */, int32_t pairs, double base, double factor,
+                          double original_length, double low_turns, double high_turns);
+
 /* ---- row gather / scatter (the 'reshape' of Sec. 4.2.1 made explicit) ---------------------------
  * gather:  dst[p, :] = src[perm[p], :]     scatter:  dst[perm[p], :] = src[p, :]
  * C * sizeof(dtype) must be a multiple of 16; src and dst must not overlap. */

@@ -14,7 +14,9 @@ from .flatten import (Geometry, shift_amount, window_tuple, pack_key, sort_tuple
                       flatten, frame_segments, Geometry3, window_tuple3, flatten3d)
 from .layer import layer_norm, gelu_erf, softmax_rows, group_layer, layer, stack
 from .pillars import point_cells, voxelize, bev_scatter
+from .attention import groups, attention, attention_backward, rotary
 
 __all__ = ["Geometry", "shift_amount", "window_tuple", "pack_key", "sort_tuple_order",
            "flatten", "frame_segments", "Geometry3", "window_tuple3", "flatten3d", "layer_norm", "gelu_erf", "softmax_rows",
-           "group_layer", "layer", "stack", "point_cells", "voxelize", "bev_scatter"]
+           "group_layer", "layer", "stack", "point_cells", "voxelize", "bev_scatter",
+           "groups", "attention", "attention_backward", "rotary"]

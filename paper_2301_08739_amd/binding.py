@@ -43,6 +43,29 @@ class VoxelGrid(C.Structure):
     _fields_ = [("x_min", C.c_float), ("y_min", C.c_float), ("voxel_x", C.c_float), ("voxel_y", C.c_float)]
 
 
+class _HeadsC(C.Structure):
+    """ff_heads"""
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _GroupListC(C.Structure):
+    """ff_group_list"""
+    _fields_ = [("perm", C.c_void_p), ("offsets", C.c_void_p), ("n", C.c_int64), ("G", C.c_int32)]
+
+
+class _AttentionShapeC(C.Structure):
+    """ff_attention_shape"""
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float),
+                ("num_groups", C.c_void_p), ("max_groups", C.c_int32), ("queries", _GroupListC), ("keys", _GroupListC),
+                ("key_mask", C.c_void_p)]
+
+
+class _RotarySpecC(C.Structure):
+    """ff_rotary_spec"""
+    _fields_ = [("axes", C.c_int32), ("pairs", C.c_int32), ("layout", C.c_int32), ("inverse", C.c_int32),
+                ("amplitude", C.c_float), ("freqs", C.c_void_p)]
+
+
 _PARAMS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_g", "ln2_b", "w1", "b1", "w2", "b2")
 
 
@@ -119,6 +142,16 @@ _SIGS = {
     "ff_fwa_block3d": (C.c_int, [C.c_void_p, C.c_int64, C.POINTER(Geometry3), C.c_int, C.c_int,
                                  C.POINTER(_LayerWeightsC), C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_size_t, C.c_void_p]),
+    "ff_attention_workspace_bytes": (C.c_size_t, [C.POINTER(_AttentionShapeC), C.c_int]),
+    "ff_attention": (C.c_int, [C.POINTER(_AttentionShapeC)] + [C.POINTER(_HeadsC)] * 4 +
+                     [C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ff_attention_backward_workspace_bytes": (C.c_size_t, [C.POINTER(_AttentionShapeC), C.c_int]),
+    "ff_attention_backward": (C.c_int, [C.POINTER(_AttentionShapeC)] + [C.POINTER(_HeadsC)] * 4 + [C.c_void_p] +
+                              [C.POINTER(_HeadsC)] * 4 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ff_rotary": (C.c_int, [C.POINTER(_HeadsC), C.POINTER(_HeadsC), C.c_int32, C.POINTER(_HeadsC), C.POINTER(_HeadsC),
+                            C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.POINTER(_RotarySpecC),
+                            C.c_int, C.c_void_p]),
+    "ff_rotary_frequencies": (C.c_int, [C.POINTER(C.c_double), C.c_int32] + [C.c_double] * 5),
     "ff_status_string": (C.c_char_p, [C.c_int]),
     "ff_version": (C.c_int, []),
 }
@@ -423,3 +456,183 @@ def ff_fwa_block(coords, geom, G, layers, dtype, feats_in, out=None, workspace=N
              *_aligned(ws), _stream())
     _check(st, name)
     return out
+
+
+# ---- attention over rows that the caller holds, and rotary positions ---------------------------------------------------
+_FF_DTYPE = {v: k for k, v in _TORCH_DTYPE.items()}
+FF_ROTARY_HALF, FF_ROTARY_INTERLEAVED = 0, 1
+
+
+def _refuse(what, why):
+    raise FlatformerError(f"{what}: {why}")
+
+
+def _heads(what, name, t, shape, dtype, device):
+    """ff_heads of a tensor [n, heads, head_dim] of any strides but the last, which is 1."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
+        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {shape} of {dtype} on {device}")
+    rs, hs, es = t.stride()
+    if es != 1 and shape[2] > 1 and t.numel():
+        _refuse(what, f"{name}: the elements of a head have to lie side by side")
+    return _HeadsC(t.data_ptr(), rs, hs)
+
+
+def _array(what, name, t, length, dtype, device):
+    """Address of a contiguous tensor of at least `length` elements; None stays None."""
+    if t is None:
+        return None
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or t.device != device or t.numel() < length or not t.is_contiguous():
+        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {length} contiguous elements of {dtype} on {device}")
+    return t.data_ptr()
+
+
+class _On:
+    """Makes a tensor's device the current one for a call, where it is not."""
+
+    def __init__(self, what, t):
+        if not t.is_cuda:
+            _refuse(what, "the tensors have to be on a GPU")
+        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return _stream()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm, key_offsets, key_G):
+    """(ff_attention_shape, ff_heads of q, of k and of v, dtype code)"""
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _FF_DTYPE:
+        _refuse(what, "q, k and v are [rows, heads, head_dim] of float32, bfloat16 or float16")
+    (nq, H, D), (nk, K, _), dev = q.shape, k.shape, q.device
+    hq = _heads(what, "q", q, (nq, H, D), q.dtype, dev)
+    hk = _heads(what, "k", k, (nk, K, D), q.dtype, dev)
+    hv = _heads(what, "v", v, (nk, K, D), q.dtype, dev)
+    if group_offsets is None:
+        _refuse(what, "group_offsets is missing")
+    i32, mg = torch.int32, int(max_groups)
+    lq = _GroupListC(_array(what, "perm", perm, nq, i32, dev), _array(what, "group_offsets", group_offsets, mg + 1, i32, dev), nq, G)
+    if key_offsets is None:
+        if key_perm is not None or key_G is not None or nk != nq:
+            _refuse(what, "keys with a list of their own need key_offsets")
+        lk = lq
+    else:
+        lk = _GroupListC(_array(what, "key_perm", key_perm, nk, i32, dev),
+                         _array(what, "key_offsets", key_offsets, mg + 1, i32, dev), nk, nk if key_G is None else key_G)
+        lk.G = max(lk.G, 1) if key_G is None else lk.G
+    s = _AttentionShapeC(H, K, D, D ** -0.5 if scale is None else scale, _array(what, "num_groups", num_groups, 1, i32, dev), mg,
+                         lq, lk, _array(what, "key_mask", key_mask, nk, (torch.uint8, torch.bool), dev))
+    return s, hq, hk, hv, _FF_DTYPE[q.dtype]
+
+
+def ff_attention_workspace_bytes(heads, kv_heads, head_dim, nq, max_groups, G, dtype, nk=None, key_G=None):
+    """Bytes that a workspace of ff_attention has to have behind its first 256-byte boundary."""
+    s = _plan_shape(heads, kv_heads, head_dim, nq, max_groups, G, nk, key_G)
+    return load_library().ff_attention_workspace_bytes(C.byref(s), dtype)
+
+
+def ff_attention_backward_workspace_bytes(heads, kv_heads, head_dim, nq, max_groups, G, dtype, nk=None, key_G=None):
+    s = _plan_shape(heads, kv_heads, head_dim, nq, max_groups, G, nk, key_G)
+    return load_library().ff_attention_backward_workspace_bytes(C.byref(s), dtype)
+
+
+def _plan_shape(heads, kv_heads, head_dim, nq, max_groups, G, nk, key_G):
+    nk = nq if nk is None else nk
+    return _AttentionShapeC(heads, kv_heads, head_dim, 1.0, None, max_groups, _GroupListC(None, None, nq, G),
+                            _GroupListC(None, None, nk, G if key_G is None else key_G), None)
+
+
+def ff_attention(q, k, v, perm, group_offsets, num_groups, max_groups, G, scale=None, key_mask=None, key_perm=None,
+                 key_offsets=None, key_G=None, out=None, lse=None, want_lse=True, workspace=None):
+    """Attention inside groups: q [nq, heads, head_dim], k and v [nk, kv_heads, head_dim], any strides with the elements of a
+    head side by side.  perm (or None), group_offsets, num_groups (or None) and max_groups are a sort's lists, or any others; keys
+    take the same ones unless key_offsets is given (key_perm, key_G: its row numbers and its longest group).  key_mask [nk],
+    uint8 or bool: 0 takes a row out.  scale: head_dim ** -0.5 unless given.  Returns (out [nq, heads, head_dim], lse float32
+    [nq, heads] or None).  Rows that no group covers are left as they were; new tensors are zero there."""
+    what = "ff_attention"
+    lib = load_library()
+    s, hq, hk, hv, dt = _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm,
+                                         key_offsets, key_G)
+    with _On(what, q) as stream:
+        if out is None:
+            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None and want_lse:
+            lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+        ho = _heads(what, "out", out, tuple(q.shape), q.dtype, q.device)
+        ws = workspace
+        if ws is None:
+            need = lib.ff_attention_workspace_bytes(C.byref(s), dt)
+            ws = _workspace(need, q.device) if need else None
+        st = lib.ff_attention(C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho),
+                              _array(what, "lse", lse, q.shape[0] * q.shape[1], torch.float32, q.device), dt,
+                              *(_aligned(ws) if ws is not None else (None, 0)), stream)
+    _check(st, what)
+    return out, lse
+
+
+def ff_attention_backward(q, k, v, out, lse, dout, perm, group_offsets, num_groups, max_groups, G, scale=None, key_mask=None,
+                          key_perm=None, key_offsets=None, key_G=None, dq=None, dk=None, dv=None, workspace=None):
+    """The gradient of ff_attention: out and lse as it gave them for the same arguments, dout the gradient of out.  Returns (dq, dk,
+    dv), like q, k and v.  Rows that no group covers are left as they were; new tensors are zero there."""
+    what = "ff_attention_backward"
+    lib = load_library()
+    s, hq, hk, hv, dt = _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm,
+                                         key_offsets, key_G)
+    shape, kshape, dev = tuple(q.shape), tuple(k.shape), q.device
+    if lse is None:
+        _refuse(what, "lse is missing")
+    with _On(what, q) as stream:
+        new = lambda t, sh: torch.zeros(sh, dtype=q.dtype, device=dev) if t is None else t  # noqa: E731
+        dq, dk, dv = new(dq, shape), new(dk, kshape), new(dv, kshape)
+        more = [_heads(what, name, t, sh, q.dtype, dev) for name, t, sh in
+                (("out", out, shape), ("dout", dout, shape), ("dq", dq, shape), ("dk", dk, kshape), ("dv", dv, kshape))]
+        ho, hg, hdq, hdk, hdv = (C.byref(m) for m in more)
+        ws = workspace
+        if ws is None:
+            need = lib.ff_attention_backward_workspace_bytes(C.byref(s), dt)
+            ws = _workspace(need, dev) if need else None
+        st = lib.ff_attention_backward(C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), ho,
+                                       _array(what, "lse", lse, shape[0] * shape[1], torch.float32, dev), hg, hdq, hdk, hdv, dt,
+                                       *(_aligned(ws) if ws is not None else (None, 0)), stream)
+    _check(st, what)
+    return dq, dk, dv
+
+
+def ff_rotary_frequencies(pairs, axes=1, base=10000.0, factor=1.0, original_length=0.0, low_turns=1.0, high_turns=32.0,
+                          device="cuda"):
+    """float64 [axes, pairs], radians a position, the same for every axis: what ff_rotary takes as freqs."""
+    f = (C.c_double * max(int(pairs), 1))()
+    _check(load_library().ff_rotary_frequencies(f, int(pairs), float(base), float(factor), float(original_length), float(low_turns),
+                                                float(high_turns)), "ff_rotary_frequencies")
+    return torch.tensor(list(f), dtype=torch.float64).repeat(axes, 1).to(device)
+
+
+def ff_rotary(q, k, positions, freqs, layout=FF_ROTARY_HALF, amplitude=1.0, inverse=False, q_out=None, k_out=None):
+    """q [n, q_heads, head_dim] and k [n, k_heads, head_dim] (or None) turned by their positions: int32 [n] or [n, axes], such as
+    coords[:, 1:], with freqs float64 [axes, pairs].  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
+    what = "ff_rotary"
+    lib = load_library()
+    if q.dim() != 3 or q.dtype not in _FF_DTYPE or (k is not None and k.dim() != 3) or freqs.dim() != 2:
+        _refuse(what, "q and k are [rows, heads, head_dim] of float32, bfloat16 or float16, freqs is [axes, pairs]")
+    (n, H, D), dev, (axes, pairs) = q.shape, q.device, freqs.shape
+    if positions.dtype != torch.int32 or positions.device != dev or tuple(positions.shape) not in ([(n,), (n, 1)] if axes == 1 else [(n, axes)]):
+        _refuse(what, f"positions: {tuple(positions.shape)} of {positions.dtype} on {positions.device}, wanted int32 {(n, axes)} on {dev}")
+    spec = _RotarySpecC(axes, pairs, layout, int(bool(inverse)), amplitude, _array(what, "freqs", freqs, axes * pairs, torch.float64, dev))
+    stride = positions.stride() + (1,)
+    with _On(what, q) as stream:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
+        hq, hqo = _heads(what, "q", q, (n, H, D), q.dtype, dev), _heads(what, "q_out", q_out, (n, H, D), q.dtype, dev)
+        hk = hko = None
+        K = 0
+        if k is not None:
+            K = k.shape[1]
+            k_out = torch.empty(k.shape, dtype=q.dtype, device=dev) if k_out is None else k_out
+            hk, hko = _heads(what, "k", k, (n, K, D), q.dtype, dev), _heads(what, "k_out", k_out, (n, K, D), q.dtype, dev)
+        st = lib.ff_rotary(hq, hqo, H, hk, hko, K, n, D, _ptr(positions), stride[0], stride[1], C.byref(spec),
+                           _FF_DTYPE[q.dtype], stream)
+    _check(st, what)
+    return q_out, k_out

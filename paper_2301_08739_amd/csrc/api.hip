@@ -1,8 +1,10 @@
 // extern "C" entry points: argument checks, workspace carving and launch order.  No kernel lives
-// here; see flatten.hip, rows.hip, layer_generic.hip, layer_mfma.hip, layer_f32.hip.
+// here; see flatten.hip, rows.hip, layer_generic.hip, layer_mfma.hip, layer_f32.hip, attention.hip, rotary.hip.
 #include "common.h"
+#include "attention.h"
 #include "pack_weights.h"
 #include <atomic>
+#include <cmath>
 
 using namespace ff;
 
@@ -32,6 +34,110 @@ bool is_16bit(int dtype) { return dtype == FF_BF16 || dtype == FF_F16; }
 bool takes_fused_path(const ff_layer_weights* w, int64_t n, int G, int dtype, uint32_t flags) {
   if (flags & FF_FLAG_FORCE_GENERIC) return false;
   return is_16bit(dtype) ? layer_mfma_supported(w, G) : layer_f32_supported(w, G) && layer_f32_pays(w, G, n);
+}
+
+
+// ---- rows of heads ----------------------------------------------------------------------------------------
+struct HeadsIn {  // one array of an entry point
+  const ff_heads* x;
+  int64_t n;
+  int32_t heads, D;
+  bool written;
+};
+
+// Elements from the first to behind the last; -1 where that passes what an address holds.
+int64_t span_elems(const HeadsIn& a) {
+  const __int128 last = (__int128)(a.n - 1) * a.x->row_stride + (__int128)(a.heads - 1) * a.x->head_stride + a.D;
+  return last > ((int64_t)1 << 60) ? -1 : (int64_t)last;
+}
+int check_heads(const HeadsIn& a, size_t size) {
+  const ff_heads* x = a.x;
+  if (!x || x->row_stride < 0 || x->head_stride < 0 || (a.n > 0 && !x->data) || (uintptr_t)x->data % size) return FF_ERR_ARG;
+  if (a.n == 0) return FF_OK;
+  if (span_elems(a) < 0) return FF_ERR_ARG;
+  if (!a.written) return FF_OK;
+  // rows outside heads, or heads outside rows
+  const __int128 row = (__int128)(a.heads - 1) * x->head_stride + a.D, head = (__int128)(a.n - 1) * x->row_stride + a.D;
+  const bool by_row = (a.heads == 1 || x->head_stride >= a.D) && (a.n == 1 || x->row_stride >= row);
+  const bool by_head = (a.n == 1 || x->row_stride >= a.D) && (a.heads == 1 || x->head_stride >= head);
+  return by_row || by_head ? FF_OK : FF_ERR_ARG;
+}
+// Do two arrays share an element?  Parts of one packed array do not: their rows (or their heads) lie at the same distances and
+// within each such distance beside each other.  What cannot be told apart so counts as shared where the ranges meet.
+bool heads_overlap(const HeadsIn& a, const HeadsIn& b, size_t size) {
+  if (a.n == 0 || b.n == 0) return false;
+  const uintptr_t x = (uintptr_t)a.x->data, y = (uintptr_t)b.x->data;
+  if (!overlaps(a.x->data, (size_t)span_elems(a) * size, b.x->data, (size_t)span_elems(b) * size)) return false;
+  const int64_t apart = (int64_t)(y - x) / (int64_t)size;  // (both are multiples of the element's size)
+  auto beside = [&](int64_t period, int64_t a_len, int64_t b_len) {  // runs of a_len and b_len elements, each once a period
+    if (period < a_len || period < b_len) return false;
+    const int64_t at = ((apart % period) + period) % period;
+    return at >= a_len && at + b_len <= period;
+  };
+  const int64_t rs = a.x->row_stride, hs = a.x->head_stride;
+  const bool rows_alike = a.n == 1 || b.n == 1 || rs == b.x->row_stride, heads_alike = a.heads == 1 || b.heads == 1 || hs == b.x->head_stride;
+  const int64_t r = a.n > 1 ? rs : b.x->row_stride, h = a.heads > 1 ? hs : b.x->head_stride;
+  if (rows_alike && beside(r, (a.heads - 1) * hs + a.D, (b.heads - 1) * b.x->head_stride + b.D)) return false;
+  if (heads_alike && beside(h, (a.n - 1) * rs + a.D, (b.n - 1) * b.x->row_stride + b.D)) return false;
+  if (rows_alike && heads_alike && h > 0 && r % h == 0 && beside(h, a.D, b.D)) return false;
+  return true;
+}
+// All arrays by themselves, and each that is written against every other one.
+int check_arrays(const HeadsIn* arrays, int count, size_t size) {
+  for (int i = 0; i < count; ++i)
+    if (const int st = check_heads(arrays[i], size); st != FF_OK) return st;
+  for (int i = 0; i < count; ++i)
+    for (int j = 0; j < count; ++j)
+      if (i != j && arrays[i].written && heads_overlap(arrays[i], arrays[j], size)) return FF_ERR_ARG;
+  return FF_OK;
+}
+// What is one piece (lists, lse, the mask, a workspace) against the arrays that are written
+bool meets_written(const HeadsIn* arrays, int count, size_t size, const void* p, size_t bytes) {
+  for (int i = 0; i < count; ++i)
+    if (arrays[i].written && arrays[i].n > 0 && overlaps(arrays[i].x->data, (size_t)span_elems(arrays[i]) * size, p, bytes)) return true;
+  return false;
+}
+Heads heads_of(const ff_heads* x) { return {x->data, x->row_stride, x->head_stride}; }
+
+int check_list(const ff_group_list& l) {
+  if (l.n < 0 || l.G < 1) return FF_ERR_ARG;
+  return l.n > INT32_MAX ? FF_ERR_UNSUPPORTED : FF_OK;
+}
+int make_attention(const ff_attention_shape* a, int dtype, Attn* out) {
+  if (!a || (dtype != FF_F32 && dtype != FF_BF16 && dtype != FF_F16)) return FF_ERR_ARG;
+  if (a->heads < 1 || a->kv_heads < 1 || a->head_dim < 1 || a->max_groups < 0 || !std::isfinite(a->scale)) return FF_ERR_ARG;
+  if (a->heads % a->kv_heads || a->head_dim > 128) return FF_ERR_UNSUPPORTED;
+  for (const ff_group_list* l : {&a->queries, &a->keys})
+    if (const int st = check_list(*l); st != FF_OK) return st;
+  auto list = [](const ff_group_list& l) { return GroupList{l.perm, l.offsets, (int32_t)l.n, l.G < l.n ? l.G : (l.n ? (int32_t)l.n : 1)}; };
+  *out = Attn{};
+  out->H = a->heads; out->K = a->kv_heads; out->D = a->head_dim;
+  out->scale = a->scale;
+  out->num_groups = a->num_groups; out->max_groups = a->max_groups;
+  out->ql = list(a->queries); out->kl = list(a->keys);
+  out->mask = a->key_mask;
+  return FF_OK;
+}
+int check_attention_call(const ff_attention_shape* a, const HeadsIn* arrays, int count, int dtype, const float* lse, bool lse_written,
+                         const void* workspace, size_t workspace_bytes, size_t need) {
+  const size_t size = elem_size(dtype), lse_bytes = (size_t)a->queries.n * a->heads * 4;
+  if (const int st = check_arrays(arrays, count, size); st != FF_OK) return st;
+  if ((a->max_groups > 0 && (!a->queries.offsets || !a->keys.offsets)) || (uintptr_t)lse % 4) return FF_ERR_ARG;
+  const struct { const void* p; size_t bytes; bool written; } pieces[] = {
+      {lse, lse_bytes, lse_written}, {workspace, need, true},
+      {a->queries.perm, (size_t)a->queries.n * 4, false}, {a->keys.perm, (size_t)a->keys.n * 4, false},
+      {a->queries.offsets, ((size_t)a->max_groups + 1) * 4, false}, {a->keys.offsets, ((size_t)a->max_groups + 1) * 4, false},
+      {a->num_groups, 4, false}, {a->key_mask, (size_t)a->keys.n, false}};
+  if (need && (!workspace || (uintptr_t)workspace % 256 || workspace_bytes < need)) return FF_ERR_WORKSPACE;
+  for (const auto& x : pieces) {
+    if (meets_written(arrays, count, size, x.p, x.bytes)) return FF_ERR_ARG;
+    for (const auto& y : pieces)
+      if (&x != &y && (x.written || y.written) && overlaps(x.p, x.bytes, y.p, y.bytes)) return FF_ERR_ARG;
+    if (x.written)
+      for (int i = 0; i < count; ++i)
+        if (arrays[i].n > 0 && overlaps(x.p, x.bytes, arrays[i].x->data, (size_t)span_elems(arrays[i]) * size)) return FF_ERR_ARG;
+  }
+  return FF_OK;
 }
 
 }  // namespace
@@ -461,6 +567,104 @@ int ff_fwa_block3d(const int32_t* coords, int64_t n, const ff_geom3* g, int G, i
   if (split_geom3(g, &g2, &z) != FF_OK) return FF_ERR_ARG;
   return fwa_block(coords, n, &g2, &z, G, tail, layers, num_layers, dtype, feats_in, feats_out, workspace,
                    workspace_bytes, stream);
+}
+
+// ---- attention over the caller's rows, rotary positions --------------------------------------------------
+size_t ff_attention_workspace_bytes(const ff_attention_shape* a, int dtype) {
+  Attn t;
+  return make_attention(a, dtype, &t) == FF_OK ? attention_workspace_bytes(t, dtype) : 0;
+}
+
+int ff_attention(const ff_attention_shape* a, const ff_heads* q, const ff_heads* k, const ff_heads* v, const ff_heads* out,
+                 float* lse, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  Attn t;
+  if (const int st = make_attention(a, dtype, &t); st != FF_OK) return st;
+  const HeadsIn arrays[] = {{q, t.ql.n, t.H, t.D, false}, {k, t.kl.n, t.K, t.D, false}, {v, t.kl.n, t.K, t.D, false},
+                            {out, t.ql.n, t.H, t.D, true}};
+  const size_t need = attention_workspace_bytes(t, dtype);
+  if (const int st = check_attention_call(a, arrays, 4, dtype, lse, true, workspace, workspace_bytes, need); st != FF_OK) return st;
+  if (t.ql.n == 0 || t.max_groups == 0) return FF_OK;
+  t.q = heads_of(q); t.k = heads_of(k); t.v = heads_of(v); t.out = heads_of(out);
+  t.lse = lse;
+  return attention_launch(t, dtype, workspace, (hipStream_t)stream);
+}
+
+size_t ff_attention_backward_workspace_bytes(const ff_attention_shape* a, int dtype) {
+  Attn t;
+  return make_attention(a, dtype, &t) == FF_OK ? attention_backward_workspace_bytes(t, dtype) : 0;
+}
+
+int ff_attention_backward(const ff_attention_shape* a, const ff_heads* q, const ff_heads* k, const ff_heads* v,
+                          const ff_heads* out, const float* lse, const ff_heads* dout, const ff_heads* dq,
+                          const ff_heads* dk, const ff_heads* dv, int dtype, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  Attn t;
+  if (const int st = make_attention(a, dtype, &t); st != FF_OK) return st;
+  if (!lse && t.ql.n > 0) return FF_ERR_ARG;
+  const HeadsIn arrays[] = {{q, t.ql.n, t.H, t.D, false}, {k, t.kl.n, t.K, t.D, false}, {v, t.kl.n, t.K, t.D, false},
+                            {out, t.ql.n, t.H, t.D, false}, {dout, t.ql.n, t.H, t.D, false}, {dq, t.ql.n, t.H, t.D, true},
+                            {dk, t.kl.n, t.K, t.D, true}, {dv, t.kl.n, t.K, t.D, true}};
+  const size_t need = attention_backward_workspace_bytes(t, dtype);
+  if (const int st = check_attention_call(a, arrays, 8, dtype, lse, false, workspace, workspace_bytes, need); st != FF_OK) return st;
+  if (t.max_groups == 0 || (t.ql.n == 0 && t.kl.n == 0)) return FF_OK;
+  t.q = heads_of(q); t.k = heads_of(k); t.v = heads_of(v); t.out = heads_of(out); t.dout = heads_of(dout);
+  t.dq = heads_of(dq); t.dk = heads_of(dk); t.dv = heads_of(dv);
+  t.lse = const_cast<float*>(lse);
+  return attention_backward_launch(t, dtype, workspace, (hipStream_t)stream);
+}
+
+int ff_rotary(const ff_heads* q, const ff_heads* q_out, int32_t q_heads, const ff_heads* k, const ff_heads* k_out,
+              int32_t k_heads, int64_t n, int32_t head_dim, const int32_t* positions, int64_t position_row_stride,
+              int64_t position_axis_stride, const ff_rotary_spec* spec, int dtype, void* stream) {
+  if (!spec || (dtype != FF_F32 && dtype != FF_BF16 && dtype != FF_F16)) return FF_ERR_ARG;
+  if (n < 0 || q_heads < 1 || k_heads < 0 || head_dim < 1 || spec->axes < 1 || spec->pairs < 1 || !spec->freqs) return FF_ERR_ARG;
+  if ((spec->layout != FF_ROTARY_HALF && spec->layout != FF_ROTARY_INTERLEAVED) || (spec->inverse != 0 && spec->inverse != 1)) return FF_ERR_ARG;
+  if (!std::isfinite(spec->amplitude) || position_row_stride < 0 || position_axis_stride < 0 || (n > 0 && !positions)) return FF_ERR_ARG;
+  if ((uintptr_t)positions % 4 || (uintptr_t)spec->freqs % 8 || (k_heads == 0) != (k == nullptr) || (k == nullptr) != (k_out == nullptr)) return FF_ERR_ARG;
+  if (spec->axes > 3 || spec->pairs > 128 || spec->axes * spec->pairs > 128 || 2 * spec->axes * spec->pairs > head_dim || head_dim > 256 || n > INT32_MAX ||
+      (int64_t)q_heads + k_heads > 65536)
+    return FF_ERR_UNSUPPORTED;
+  const size_t size = elem_size(dtype);
+  const HeadsIn arrays[] = {{q, n, q_heads, head_dim, false}, {q_out, n, q_heads, head_dim, true},
+                            {k, n, k_heads, head_dim, false}, {k_out, n, k_heads, head_dim, true}};
+  const int count = k ? 4 : 2;
+  for (int i = 0; i < count; ++i)
+    if (const int st = check_heads(arrays[i], size); st != FF_OK) return st;
+  auto same = [](const ff_heads* a, const ff_heads* b) { return a->data == b->data && a->row_stride == b->row_stride && a->head_stride == b->head_stride; };
+  for (int i = 0; i < count; ++i)
+    for (int j = 0; j < count; ++j)
+      if (i != j && arrays[i].written && !(j == i - 1 && same(arrays[i].x, arrays[j].x)) && heads_overlap(arrays[i], arrays[j], size)) return FF_ERR_ARG;
+  const __int128 last = (__int128)(n - 1) * position_row_stride + (__int128)(spec->axes - 1) * position_axis_stride + 1;
+  if (n > 0 && last > ((int64_t)1 << 60)) return FF_ERR_ARG;
+  if (n > 0 && (meets_written(arrays, count, size, positions, (size_t)last * 4) ||
+                meets_written(arrays, count, size, spec->freqs, (size_t)spec->axes * spec->pairs * 8)))
+    return FF_ERR_ARG;
+  if (n == 0) return FF_OK;
+  Rotary r{};
+  r.q = heads_of(q); r.q_out = heads_of(q_out);
+  if (k) { r.k = heads_of(k); r.k_out = heads_of(k_out); }
+  r.q_heads = q_heads; r.k_heads = k_heads; r.D = head_dim; r.n = n;
+  r.pos = positions; r.pos_rs = position_row_stride; r.pos_as = position_axis_stride;
+  r.freqs = spec->freqs; r.axes = spec->axes; r.pairs = spec->pairs; r.layout = spec->layout;
+  r.sign = spec->inverse ? -1.f : 1.f; r.amplitude = spec->amplitude;
+  return rotary_launch(r, dtype, (hipStream_t)stream);
+}
+
+int ff_rotary_frequencies(double* freqs, int32_t pairs, double base, double factor, double original_length,
+                          double low_turns, double high_turns) {
+  if (!freqs || pairs < 1 || !(base > 0) || !std::isfinite(base) || !(factor > 0) || !std::isfinite(factor)) return FF_ERR_ARG;
+  if (!(original_length >= 0) || !std::isfinite(original_length) || !std::isfinite(low_turns) || !std::isfinite(high_turns) || !(high_turns > low_turns))
+    return FF_ERR_ARG;
+  for (int32_t i = 0; i < pairs; ++i) {
+    const double f = std::pow(base, -(double)i / pairs);
+    double w = 0.0;
+    if (original_length > 0) {
+      w = (original_length * f / 6.283185307179586477 - low_turns) / (high_turns - low_turns);
+      w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+    }
+    freqs[i] = f * (w + (1.0 - w) / factor);
+  }
+  return FF_OK;
 }
 
 const char* ff_status_string(int status) {

@@ -1,0 +1,333 @@
+"""GPU: ff_attention and ff_attention_backward against the float64 oracle, within the oracle's bounds on what rounding costs (half a
+step of the type for each rounding, float32 sums), times no factor."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2301_08739_amd as ff
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+class Case:
+    """Rows, lists and what ff_attention is called with."""
+
+    def __init__(self, dtype, lens_q, lens_k=None, H=2, K=2, D=16, seed=0, masked=None, layout="plain", shuffle=True, spare=0,
+                 gap=0, big=1.0, G=None, key_G=None):
+        rng = np.random.default_rng(seed)
+        self.dtype, self.H, self.K, self.D = dtype, H, K, D
+        self.cross = lens_k is not None
+        lens_k = lens_k if self.cross else lens_q
+        self.nq, self.nk = sum(lens_q) + gap, sum(lens_k) + gap
+        self.ng, self.max_groups = len(lens_q), len(lens_q) + spare
+        self.scale = 1.0 / np.sqrt(D)
+
+        def a_list(lens, n):
+            off = np.full(self.max_groups + 1, -1, np.int32)
+            off[:self.ng + 1] = np.concatenate([[0], np.cumsum(lens)])
+            return (rng.permutation(n) if shuffle else np.arange(n)).astype(np.int32), off
+
+        self.perm, self.off = a_list(lens_q, self.nq)
+        self.kperm, self.koff = a_list(lens_k, self.nk) if self.cross else (self.perm, self.off)
+        self.G = max(max(lens_q, default=1), 1) if G is None else G
+        self.key_G = (max(max(lens_k, default=1), 1) if key_G is None else key_G) if self.cross else self.G
+        self.mask = None
+        if masked is not None:
+            self.mask = (rng.random(self.nk) >= masked).astype(np.uint8)
+        t = TYPES[dtype]
+        make = lambda n, h: torch.from_numpy(big * rng.standard_normal((n, h, D))).to(t).to(DEV)
+        self.q, self.k, self.v, self.g = make(self.nq, H), make(self.nk, K), make(self.nk, K), make(self.nq, H)
+        lay = {"plain": self._plain, "packed": self._packed, "heads_first": self._heads_first, "odd": self._odd}[layout]
+        self.place = lay
+        self.q, self.k, self.v, self.g = (lay(x) for x in (self.q, self.k, self.v, self.g))
+
+    @staticmethod
+    def _plain(x):
+        return x
+
+    @staticmethod
+    def _packed(x):                                   # one of several arrays side by side
+        big = torch.full((x.shape[0], 3 * x.shape[1], x.shape[2]), 7.0, dtype=x.dtype, device=DEV)
+        view = big[:, x.shape[1]:2 * x.shape[1]]
+        return view.copy_(x)
+
+    @staticmethod
+    def _heads_first(x):
+        return x.transpose(0, 1).contiguous().transpose(0, 1)
+
+    @staticmethod
+    def _odd(x):                                      # rows that begin anywhere
+        big = torch.full((x.shape[0], x.shape[1], x.shape[2] + 3), 7.0, dtype=x.dtype, device=DEV)
+        view = big[:, :, 1:1 + x.shape[2]]
+        return view.copy_(x)
+
+    def lists(self):
+        dev = lambda a: torch.from_numpy(a).to(DEV)
+        args = (dev(self.perm), dev(self.off), torch.tensor([self.ng], dtype=torch.int32, device=DEV), self.max_groups, self.G)
+        more = dict(scale=self.scale, key_mask=None if self.mask is None else dev(self.mask))
+        if self.cross:
+            more.update(key_perm=dev(self.kperm), key_offsets=dev(self.koff), key_G=self.key_G)
+        return args, more
+
+    def groups(self):
+        return (oracle.groups(self.perm, self.off, self.ng, self.nq, self.G),
+                oracle.groups(self.kperm, self.koff, self.ng, self.nk, self.key_G))
+
+    def host(self, t):
+        return t.detach().double().cpu().numpy()
+
+    def run(self, backward=True, **kw):
+        args, more = self.lists()
+        like = lambda x: self.place(torch.full(x.shape, 5.0, dtype=x.dtype, device=DEV))
+        out, lse = like(self.q), torch.full((self.nq, self.H), 5.0, device=DEV)
+        ff.ff_attention(self.q, self.k, self.v, *args, out=out, lse=lse, **more, **kw)
+        if not backward:
+            return out, lse
+        grads = [like(x) for x in (self.q, self.k, self.v)]
+        ff.ff_attention_backward(self.q, self.k, self.v, out, lse, self.g, *args, **more, dq=grads[0], dk=grads[1], dv=grads[2])
+        torch.cuda.synchronize()
+        return (out, lse, *grads)
+
+    def check(self, backward=True):
+        got = self.run(backward)
+        x = [self.host(t) for t in (self.q, self.k, self.v)]
+        qg, kg = self.groups()
+        out, lse, ob, lb = oracle.attention(*x, qg, kg, self.scale, self.mask, self.dtype)
+        pairs = [("out", got[0], out, ob), ("lse", got[1], lse, lb)]
+        if backward:
+            grads, bounds = oracle.attention_backward(*x, self.host(self.g), qg, kg, self.scale, self.mask, self.dtype)
+            pairs += list(zip(("dq", "dk", "dv"), got[2:], grads, bounds))
+        for name, mine, want, bound in pairs:
+            mine = self.host(mine)
+            assert (mine[np.isnan(want)] == 5.0).all(), name + ": rows of no group"
+            there = ~np.isnan(want)
+            mine, want, bound = mine[there], want[there], bound[there]
+            with np.errstate(invalid="ignore"):
+                ok = (mine == want) | (np.abs(mine - want) <= bound)
+            assert ok.all(), (name, int((~ok).sum()), float(np.nanmax(np.where(ok, 0, np.abs(mine - want)))), mine[~ok][:4], want[~ok][:4])
+
+
+DIMS = [1, 5, 8, 16, 24, 32, 40, 64, 72, 80, 96, 104, 128]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", DIMS)
+def test_head_sizes(dtype, D):
+    Case(dtype, [64, 1, 33, 100], D=D, seed=D).check()
+    Case(dtype, [200, 3], D=D, seed=D, H=4, K=2).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[1], [1] * 70, [2, 0, 5, 0, 0, 1], [15, 16, 17], [31, 32, 33], [63, 64, 65], [127, 128, 129], [255, 256, 257],
+                                  [69] * 20 + [11], [513, 1, 40], [0], [0, 0, 3], [1500, 7, 0, 800]], ids=lambda l: "-".join(map(str, l[:4])))
+@pytest.mark.parametrize("D", [16, 64])
+def test_lengths(dtype, lens, D):
+    Case(dtype, lens, D=D, seed=len(lens), spare=3).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,K", [(1, 1), (3, 3), (3, 1), (8, 2), (6, 3), (5, 5), (16, 16)])
+def test_shared_heads(dtype, H, K):
+    Case(dtype, [40, 70], H=H, K=K, D=16, seed=H).check()
+    Case(dtype, [40, 150], H=H, K=K, D=32, seed=H).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [([1], [1]), ([1], [4000]), ([3, 1], [0, 700]), ([0, 2], [5, 0]), ([200], [2500]), ([1, 1, 1, 1], [900, 1, 33, 3000]),
+                                  ([2500], [3]), ([700, 20], [1, 90]), ([17], [129])], ids=str)
+@pytest.mark.parametrize("D", [16, 40, 128])
+def test_queries_over_other_rows(dtype, lens, D):
+    Case(dtype, *lens, H=4, K=2, D=D, seed=7).check()
+    Case(dtype, *lens, H=4, K=4, D=D, seed=8, masked=0.5).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["packed", "heads_first", "odd"])
+@pytest.mark.parametrize("D", [16, 24, 64])
+def test_strides(dtype, layout, D):
+    Case(dtype, [64, 20, 130], H=4, K=2, D=D, layout=layout, seed=3).check()
+    Case(dtype, [64, 20, 1], H=4, K=4, D=D, layout=layout, seed=3).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[50, 64, 10], [300, 20]], ids=str)
+@pytest.mark.parametrize("D", [16, 64])
+def test_masked_rows_may_hold_anything(dtype, lens, D):
+    c = Case(dtype, lens, D=D, masked=0.4, seed=5)
+    c.mask[c.kperm[:lens[0]]] = 0                     # the first group has no key left
+    out = torch.from_numpy(np.flatnonzero(c.mask == 0)).to(DEV)
+    for x, bad in ((c.k, float("nan")), (c.v, float("inf"))):
+        x[out] = bad
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens", [[30, 40], [300, 20]], ids=str)
+def test_rows_that_no_group_covers_stay(dtype, lens):
+    Case(dtype, lens, gap=9, seed=6).check()
+    Case(dtype, lens, gap=9, seed=6, G=25).check()    # groups cut at G positions, as in a list of dropped tails
+    Case(dtype, lens, [70, 12], gap=3, seed=6, G=25, key_G=50).check()
+
+
+@pytest.mark.parametrize("lens", [[30, 40], [300, 20]], ids=str)
+def test_lists_that_leave_the_rows(lens):
+    """Offsets outside the rows are cut, rows that there are none of are passed over."""
+    c = Case("f32", lens, seed=9)
+    n = c.nq
+    c.off[-1] = n + 1000
+    c.off[0] = -5
+    c.perm[3], c.perm[n - 2] = n + 7, -1
+    c.G = n + 50
+    c.check()
+    c.ng = -1
+    out, lse, *grads = c.run()
+    assert all((t == 5.0).all() for t in (out, lse, *grads))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("big", [4.0, 12.0])
+def test_peaked_scores(dtype, big):
+    Case(dtype, [64, 300], D=32, big=big, seed=10).check()
+
+
+@pytest.mark.parametrize("D,lens", [(16, [40, 64]), (64, [300])])
+@pytest.mark.parametrize("scale", [0.0, -0.5, 30.0])
+def test_scales(D, lens, scale):
+    c = Case("f32", lens, D=D, seed=11)
+    c.scale = scale
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,lens", [(16, [40, 64]), (64, [300, 5])])
+def test_infinities_and_nans_in_their_own_group_only(dtype, D, lens):
+    c = Case(dtype, lens, D=D, seed=12)
+    want = c.run()
+    first = torch.from_numpy(c.perm[:lens[0]].astype(np.int64)).to(DEV)
+    rest = torch.from_numpy(c.perm[lens[0]:].astype(np.int64)).to(DEV)
+    c.v[first[1], 0, 2] = float("inf")
+    out, lse, *_ = got = c.run()
+    assert torch.isinf(out[first, 0, 2]).all() and torch.isfinite(out[first, 0, 3]).all()
+    assert torch.equal(lse, want[1])
+    for a, b in zip(got, want):
+        assert torch.equal(a[rest], b[rest])
+    c.k[first[2], 1, 0] = float("nan")
+    got = c.run()
+    assert torch.isnan(got[0][first, 1]).all() and torch.isnan(got[1][first, 1]).all()
+    for a, b in zip(got, want):
+        assert torch.equal(a[rest], b[rest])
+
+
+@pytest.mark.parametrize("dtype,D,lens,lens_k", [("bf16", 16, [64] * 9 + [5], None), ("f16", 64, [500, 40], None), ("f32", 32, [3, 5], [3000, 900])])
+def test_same_bits_eagerly_on_a_stream_and_in_graphs(dtype, D, lens, lens_k):
+    """Two captured calls share one workspace; replays with eager work and new inputs between them."""
+    c = Case(dtype, lens, lens_k, H=4, K=2, D=D, seed=13)
+    want = [t.clone() for t in c.run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = c.run()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+    args, more = c.lists()
+    sizes = (c.H, c.K, D, c.nq, c.max_groups, c.G, {"f32": ff.FF_F32, "bf16": ff.FF_BF16, "f16": ff.FF_F16}[dtype], c.nk, c.key_G)
+    need = max(ff.ff_attention_workspace_bytes(*sizes), ff.ff_attention_backward_workspace_bytes(*sizes))
+    ws = torch.empty(need + 512, dtype=torch.uint8, device=DEV)
+    bufs = [torch.zeros_like(t) for t in want]
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        ff.ff_attention(c.q, c.k, c.v, *args, out=bufs[0], lse=bufs[1], workspace=ws, **more)
+    with torch.cuda.graph(graphs[1]):
+        ff.ff_attention_backward(c.q, c.k, c.v, bufs[0], bufs[1], c.g, *args, dq=bufs[2], dk=bufs[3], dv=bufs[4], workspace=ws, **more)
+    for _ in range(3):
+        for b in bufs:
+            b.fill_(3.0)
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        covered = [c.perm[:sum(lens)]] * 3 + [c.kperm[:c.koff[c.ng]]] * 2
+        for b, w, rows in zip(bufs, want, covered):
+            r = torch.from_numpy(rows.astype(np.int64)).to(DEV)
+            assert torch.equal(b[r], w[r])
+    c.q.mul_(0.5)
+    want = c.run()
+    for graph in graphs:
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(bufs, want))
+
+
+@pytest.mark.parametrize("D", [16, 64])
+def test_broadcast_keys_and_their_gradient(D):
+    """One key and value head, spread over all heads by strides of zero; the gradient goes to heads of its own."""
+    c = Case("f32", [64, 130], H=4, K=4, D=D, seed=14)
+    c.k, c.v = (x[:, :1].expand(-1, 4, -1) for x in (c.k, c.v))
+    c.check()
+    one = Case("f32", [64, 130], H=4, K=1, D=D, seed=14)
+    one.q, one.g, one.perm, one.off = c.q, c.g, c.perm, c.off
+    one.k, one.v = c.k[:, :1].contiguous(), c.v[:, :1].contiguous()
+    a, b = c.run(), one.run()
+    for i in (3, 4):                                   # sums over 4 x 130 products, in other orders
+        assert torch.allclose(a[i].sum(1), b[i][:, 0], rtol=1e-4, atol=1e-4)
+
+
+def test_gradient_against_differences():
+    c = Case("f32", [50, 200], H=4, K=2, D=32, seed=15)
+    args, more = c.lists()
+    out, lse, *grads = c.run()
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    x = [c.q, c.k, c.v]
+    h = 2.0 ** -7
+    for i in range(3):
+        d = torch.randn(x[i].shape, device=DEV, generator=gen)
+        loss = []
+        for s in (h, -h):
+            y = [t + s * d if j == i else t for j, t in enumerate(x)]
+            loss.append((ff.ff_attention(*y, *args, **more)[0].double() * c.g.double()).sum())
+        slope, want = ((loss[0] - loss[1]) / (2 * h)).item(), (grads[i].double() * d.double()).sum().item()
+        size = (grads[i].double() * d.double()).norm().item()       # third derivatives: h^2 of it; rounding: 2^-24 / h of the loss
+        assert abs(slope - want) < 0.02 * size + 1e-3, (i, slope, want, size)
+
+
+@pytest.mark.parametrize("dtype,n,G,tail", [("bf16", 3000, 64, ff.FF_TAIL_MASK), ("f32", 1000, 32, ff.FF_TAIL_DROP), ("f16", 2100, 69, ff.FF_TAIL_DROP)])
+def test_a_layer_of_the_users_own(cfg, dtype, n, G, tail):
+    """Sort, positions, attention, its gradient and the positions' gradient together, against the chain in float64."""
+    cloud = cfg(2)
+    coords = torch.from_numpy(np.ascontiguousarray(cloud["coords"][:n])).to(DEV)
+    geom = ff.Geometry(1, cloud["grid"], cloud["grid"], cloud["window"], cloud["window"])
+    perm, off, ng, _ = ff.ff_flatten(coords, geom, 0, 0, G, tail=tail)
+    H, D = 4, 16
+    rng = np.random.default_rng(16)
+    t = TYPES[dtype]
+    qkv = torch.from_numpy(rng.standard_normal((n, 3, H, D))).to(t).to(DEV)
+    g = torch.from_numpy(rng.standard_normal((n, H, D))).to(t).to(DEV)
+    q, k, v = qkv.unbind(1)
+    freqs = ff.ff_rotary_frequencies(D // 4, axes=2, base=100.0)
+    q2, k2 = ff.ff_rotary(q, k, coords[:, 1:], freqs)
+    lists = (perm, off, ng, -(-n // G), G)
+    out, lse = ff.ff_attention(q2, k2, v, *lists)
+    grads = torch.zeros_like(qkv)
+    dq, dk, dv = grads.unbind(1)
+    ff.ff_attention_backward(q2, k2, v, out, lse, g, *lists, dq=dq, dk=dk, dv=dv)
+    ff.ff_rotary(dq, dk, coords[:, 1:], freqs, inverse=True, q_out=dq, k_out=dk)
+    host = lambda x: x.detach().double().cpu().numpy()
+    groups = oracle.groups(perm.cpu().numpy(), off.cpu().numpy(), int(ng.item()), n, G)
+    p, f = coords[:, 1:].cpu().numpy(), freqs.cpu().numpy()
+    rq, rk = (oracle.rotary(host(x), p, f, True) for x in (q, k))
+    want, _, _, _ = oracle.attention(rq, rk, host(v), groups, groups, D ** -0.5)
+    (wq, wk, wv), _ = oracle.attention_backward(rq, rk, host(v), host(g), groups, groups, D ** -0.5)
+    wq, wk = (oracle.rotary(x, p, f, True, inverse=True) for x in (wq, wk))
+    # each operator rounds what it hands on: in all some ten half steps of values near one, of which scores pass on their size
+    step = 32 * {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype]
+    for name, mine, ref in (("out", out, want), ("dq", dq, wq), ("dk", dk, wk), ("dv", dv, wv)):
+        mine, there = host(mine), ~np.isnan(ref)
+        assert (mine[~there] == 0).all(), name
+        err = np.linalg.norm((mine - ref)[there]) / np.linalg.norm(ref[there])
+        assert err < step / 4 and np.abs((mine - ref)[there]).max() < step * max(1.0, np.abs(ref[there]).max()), (name, err)
