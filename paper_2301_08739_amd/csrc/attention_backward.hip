@@ -1,65 +1,10 @@
-// Attention over the caller's rows and its gradient: the plain kernels.  A wavefront takes one query (or one key) of one head and
+// The gradient of attention over the caller's rows: plain kernels.  A wavefront takes one query (or one key) of one head and
 // goes through the rows of the other side 64 at a time: a lane a row for the scores, a lane two elements for the sums.  Right for
 // every shape; bound by instruction issue and by rows that every wavefront reads again.
 #include "attention.h"
 
 namespace ff {
 namespace {
-
-constexpr int kMaxDim = 128;
-
-template <typename T> __device__ __forceinline__ float dot(const float* a, const T* b, int D) {
-  float s = 0.f;
-  for (int e = 0; e < D; ++e) s = fmaf(a[e], Elem<T>::load(b + e), s);
-  return s;
-}
-
-template <typename T> __global__ __launch_bounds__(64) void k_attention_plain(Attn a) {
-  __shared__ float qs[kMaxDim], ps[64];
-  __shared__ int32_t rows[64];
-  const int lane = threadIdx.x, h = blockIdx.y, kh = h / (a.H / a.K);
-  const int g = blockIdx.x / a.ql.G, i = blockIdx.x % a.ql.G;
-  if (g >= groups_of(a)) return;
-  const Span sq = span_of(a.ql, g), sk = span_of(a.kl, g);
-  if (i >= sq.len) return;
-  const int32_t row = row_at(a.ql, sq.at + i);
-  if (row < 0) return;
-  const T* q = row_of_head<T>(a.q, row, h);
-  for (int e = lane; e < a.D; e += 64) qs[e] = Elem<T>::load(q + e);
-  __syncthreads();
-  float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
-  bool any = false;
-  for (int j0 = 0; j0 < sk.len; j0 += 64) {
-    const int32_t r = j0 + lane < sk.len ? row_at(a.kl, sk.at + j0 + lane) : -1;
-    const bool ok = r >= 0 && (!a.mask || a.mask[r]);
-    const float s = ok ? a.scale * dot(qs, row_of_head<T>(a.k, r, kh), a.D) : -INFINITY;
-    any |= __any(ok);
-    float m = s;
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    m = fmaxf(m, top);
-    const float base = m == -INFINITY ? 0.f : m, p = ok ? expf(s - base) : 0.f, f = expf(top - base);
-    float t = p;
-    for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d);
-    sum = sum * f + t;
-    top = m;
-    ps[lane] = p;
-    rows[lane] = ok ? r : -1;
-    __syncthreads();
-    o0 *= f;
-    o1 *= f;
-    for (int j = 0; j < 64; ++j) {
-      if (rows[j] < 0) continue;
-      const T* v = row_of_head<T>(a.v, rows[j], kh);
-      if (lane < a.D) o0 = fmaf(ps[j], Elem<T>::load(v + lane), o0);
-      if (lane + 64 < a.D) o1 = fmaf(ps[j], Elem<T>::load(v + lane + 64), o1);
-    }
-    __syncthreads();
-  }
-  T* out = row_of_head<T>(a.out, row, h);
-  if (lane < a.D) Elem<T>::store(out + lane, any ? o0 / sum : 0.f);
-  if (lane + 64 < a.D) Elem<T>::store(out + lane + 64, any ? o1 / sum : 0.f);
-  if (lane == 0 && a.lse) a.lse[(int64_t)row * a.H + h] = any ? top + logf(sum) : -INFINITY;
-}
 
 // p and e of one (query, key) pair of rows
 template <typename T>
@@ -155,12 +100,6 @@ template <typename T> __global__ __launch_bounds__(64) void k_attention_dkv_plai
   }
 }
 
-template <typename T> int forward(const Attn& a, hipStream_t stream) {
-  const int64_t slots = (int64_t)a.max_groups * a.ql.G;
-  if (slots > INT32_MAX || a.H > 65535) return FF_ERR_UNSUPPORTED;
-  k_attention_plain<T><<<dim3((uint32_t)slots, a.H), 64, 0, stream>>>(a);
-  return launch_status();
-}
 template <typename T> int backward(const Attn& a, hipStream_t stream) {
   const int64_t sq = (int64_t)a.max_groups * a.ql.G, sk = (int64_t)a.max_groups * a.kl.G;
   if (sq > INT32_MAX || sk > INT32_MAX || a.H > 65535) return FF_ERR_UNSUPPORTED;
@@ -171,11 +110,7 @@ template <typename T> int backward(const Attn& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t attention_workspace_bytes(const Attn&, int) { return 0; }
 size_t attention_backward_workspace_bytes(const Attn&, int) { return 0; }
-int attention_launch(const Attn& a, int dtype, void*, hipStream_t stream) {
-  return dtype == FF_F32 ? forward<float>(a, stream) : dtype == FF_BF16 ? forward<bf16_t>(a, stream) : forward<f16_t>(a, stream);
-}
 int attention_backward_launch(const Attn& a, int dtype, void*, hipStream_t stream) {
   return dtype == FF_F32 ? backward<float>(a, stream) : dtype == FF_BF16 ? backward<bf16_t>(a, stream) : backward<f16_t>(a, stream);
 }

@@ -1,0 +1,218 @@
+// Matrix-core pieces of the attention kernels, alike for bfloat16, half and float32.
+//
+// Every product is made of 16 x 16 tiles.  An operand piece holds 16 bytes a lane: lane (g, i) = (lane / 16, lane % 16) has, of row i
+// of the operand (a column of the right one), the KF / 4 elements from k = g * KF / 4 on; KF is 32 for 16-bit types (one instruction)
+// and 16 for float32 (four, one an element: the order of k is another one on both sides alike).  A result tile holds rows 4 g .. 4 g + 3
+// of column i.  So where a product's result is next summed over its rows, it becomes the right operand of the next product as it
+// lies in the registers: a piece of KF rows is KF / 16 tiles one after the other, and the left operand is read in that order of k,
+// from LDS, down its columns (16 bits: the transposing read; float32: element by element).
+#pragma once
+#include "attention.h"
+
+namespace ff {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kLowest = -3.402823466e38f;
+
+union Piece {  // 16 bytes of an operand
+  u32x4 q;
+  f32x4 f;
+  b16x8 b;
+  h16x8 h;
+  s16x4 s[2];
+  b16x4 b4[2];
+  h16x4 h4[2];
+};
+
+template <typename T> struct Mx {
+  static constexpr int KF = 32, E = 8, TILES = 2;
+};
+template <> struct Mx<float> {
+  static constexpr int KF = 16, E = 4, TILES = 1;
+};
+
+template <typename T> __device__ __forceinline__ f32x4 mma(const Piece& a, const Piece& b, f32x4 c);
+template <> __device__ __forceinline__ f32x4 mma<bf16_t>(const Piece& a, const Piece& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.b, b.b, c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 mma<f16_t>(const Piece& a, const Piece& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.h, b.h, c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 mma<float>(const Piece& a, const Piece& b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[j], b.f[j], c, 0, 0, 0);
+  return c;
+}
+
+// TILES result tiles as the right operand of the next product, rounded to the type (to nearest even)
+template <typename T> __device__ __forceinline__ Piece as_piece(const f32x4* t);
+template <> __device__ __forceinline__ Piece as_piece<bf16_t>(const f32x4* t) {
+  Piece p;
+  p.b4[0] = __builtin_convertvector(t[0], b16x4);
+  p.b4[1] = __builtin_convertvector(t[1], b16x4);
+  return p;
+}
+template <> __device__ __forceinline__ Piece as_piece<f16_t>(const f32x4* t) {
+  Piece p;
+  p.h4[0] = __builtin_convertvector(t[0], h16x4);
+  p.h4[1] = __builtin_convertvector(t[1], h16x4);
+  return p;
+}
+template <> __device__ __forceinline__ Piece as_piece<float>(const f32x4* t) {
+  Piece p;
+  p.f = t[0];
+  return p;
+}
+
+// Four elements side by side (one lane's part of a result tile) into memory, those from D on left out
+template <typename T> __device__ __forceinline__ void store4(T* row, int e, f32x4 v, int D, bool whole) {
+  if (whole) {
+    if (e >= D) return;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<f32x4*>(row + e) = v;
+    } else {
+      const f32x4 t[2] = {v, v};
+      const Piece p = as_piece<T>(t);
+      *reinterpret_cast<s16x4*>(row + e) = p.s[0];
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (e + r < D) Elem<T>::store(row + e + r, v[r]);
+  }
+}
+
+// 16 bytes of a row from element e on, zero from D on.  whole: rows are 16-byte pieces, from their addresses to their ends.
+template <typename T> __device__ __forceinline__ Piece load_piece(const T* row, int e, int D, bool whole) {
+  Piece p;
+  p.q = u32x4{0u, 0u, 0u, 0u};
+  if (whole) {
+    if (e < D) p.q = *reinterpret_cast<const u32x4*>(row + e);
+  } else {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e + j < D) p.f[j] = row[e + j];
+    } else {
+      const uint16_t* x = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (e + j < D) p.q[j / 2] |= (uint32_t)x[e + j] << (16 * (j % 2));
+    }
+  }
+  return p;
+}
+
+// The piece down column d0 + i of an LDS tile: rows r0 + 16 t + 4 g + j for tiles t < TILES, in the order of as_piece
+template <typename T> __device__ __forceinline__ Piece column_piece(const T* tile, int ld, int r0, int d0, int lane) {
+  Piece p;
+  const int g = lane >> 4, i = lane & 15;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p.f[j] = tile[(r0 + 4 * g + j) * ld + d0 + i];
+  } else {
+    // sixteen lanes read four rows of sixteen elements, 8 bytes a lane, and get a column of four each
+    const T* at = tile + (r0 + 4 * g + (i >> 2)) * ld + d0 + (i & 3) * 4;
+    p.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    p.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * ld));
+  }
+  return p;
+}
+template <typename T> __device__ __forceinline__ Piece row_piece(const T* tile, int ld, int r, int e) {
+  Piece p;
+  p.q = *reinterpret_cast<const u32x4*>(tile + r * ld + e);
+  return p;
+}
+
+// What lanes of a wavefront wrote into LDS is there for its other lanes
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float over_lanes16_max(float v) {  // over the four lanes of a column
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float over_lanes16_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// ---- which tile of which group ---------------------------------------------------------------------------
+// Tiles of B rows (positions times `share` heads that have their keys in common).  Groups of about the same length: tile t is tile
+// t % per_group of group t / per_group.  Else, so that long lists of mostly short groups launch few empty workgroups: group g owns
+// tiles floor(offsets[g] * share / B) + g and on, which is at least as many as it has, whatever the lengths, and a wavefront finds
+// the group of a tile in two or three looks at 64 offsets.
+struct TileGrid {
+  int32_t tiles, per_group, share;  // per_group 0: by offsets
+};
+struct TileAt {
+  int32_t g, tile;  // g < 0: none
+};
+template <int B> __device__ __forceinline__ TileAt tile_at(const Attn& a, const GroupList& l, const TileGrid& tg, int32_t t, int lane) {
+  const int32_t ng = groups_of(a);
+  if (ng <= 0) return {-1, 0};
+  if (tg.per_group) {
+    const int32_t g = t / tg.per_group;
+    return {g < ng ? g : -1, t - g * tg.per_group};
+  }
+  auto base = [&](int32_t g) { return (int32_t)((int64_t)clamp_to(l.off[g], l.n) * tg.share / B) + g; };
+  int32_t lo = 0, hi = ng;
+  while (hi - lo > 1) {
+    const int32_t step = (hi - lo + 63) / 64, g = lo + lane * step;
+    const int below = __popcll(__ballot(g < hi && base(g) <= t));
+    lo += (below > 0 ? below - 1 : 0) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  const int32_t first = base(lo);
+  return {first <= t ? lo : -1, t - first};
+}
+inline TileGrid tile_grid(int64_t n, int64_t G, int64_t share, int64_t max_groups, int64_t B, bool* fits) {
+  const int64_t per = ceil_div(G * share, B), even = per * max_groups, by_offsets = n * share / B + max_groups + 1;
+  const bool direct = even <= by_offsets + by_offsets / 2;
+  const int64_t tiles = direct ? even : by_offsets;
+  *fits = tiles <= INT32_MAX;
+  return {(int32_t)(*fits ? tiles : 0), direct ? (int32_t)per : 0, (int32_t)share};
+}
+
+// ---- a tile of rows into LDS ------------------------------------------------------------------------------
+template <typename T, int DP, int R, int NT> struct Rows {
+  static constexpr int PER = DP * (int)sizeof(T) / 16;              // pieces of a row
+  static constexpr int U = (R * PER + NT - 1) / NT;                 // pieces of a thread
+  static constexpr int STEP = NT / PER;                             // rows between two pieces of a thread
+  static __device__ __forceinline__ int row(int tid, int u) { return tid / PER + u * STEP; }
+  static __device__ __forceinline__ void fetch(Piece (&r)[U], const Heads& x, const int32_t (&rows)[U], const int32_t (&heads)[U], int tid,
+                                               int D, bool whole) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      r[u].q = u32x4{0u, 0u, 0u, 0u};
+      if (rows[u] >= 0) r[u] = load_piece(row_of_head<const T>(x, rows[u], heads[u]), (tid % PER) * Mx<T>::E, D, whole);
+    }
+  }
+  static __device__ __forceinline__ void put(T* tile, int ld, const Piece (&r)[U], int tid) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (R * PER % NT == 0 || row(tid, u) < R) *reinterpret_cast<u32x4*>(tile + row(tid, u) * ld + (tid % PER) * Mx<T>::E) = r[u].q;
+  }
+};
+
+// May rows of this array be read and written in pieces of 16 bytes?
+inline bool whole_pieces(const Heads& x, int D, size_t size) {
+  return ((uintptr_t)x.p | (uintptr_t)(x.rs * size) | (uintptr_t)(x.hs * size) | (uintptr_t)(D * size)) % 16 == 0;
+}
+
+}  // namespace
+}  // namespace ff
