@@ -76,7 +76,9 @@ def attention_backward(q, k, v, dout, qg, kg, scale, mask=None, dtype="f32"):
             e = p * (dp - delta)
             off = ((D + 2) * U32 * abs(scale) * (np.abs(a) @ np.abs(b).T)).max(1, keepdims=True) + 4 * U32 * np.abs(s).max(1, keepdims=True)
             rel = 2 * (off + lse_bound[rq, h][:, None] + 8 * U32)
-            e_off = p * ((D + 2) * U32 * (dp_abs + (np.abs(g) * np.abs(out[rq, h])).sum(1, keepdims=True)) +
+            # float32's exponential ends at its smallest normal number: p is off by 2^-126 beside its relative error, and e = p (dp - delta)
+            # by that times |dp - delta| <= sum |g v| + |delta|
+            e_off = 2.0 ** -126 * (dp_abs + np.abs(delta)) + p * ((D + 2) * U32 * (dp_abs + (np.abs(g) * np.abs(out[rq, h])).sum(1, keepdims=True)) +
                          (np.abs(g) * out_bound[rq, h]).sum(1, keepdims=True))
             e_bound = (u + rel) * (np.abs(e) + e_off) + e_off + tiny
             p_bound = (u + rel) * p + tiny

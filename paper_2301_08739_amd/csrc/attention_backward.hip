@@ -1,118 +1,694 @@
-// The gradient of attention over the caller's rows: plain kernels.  A wavefront takes one query (or one key) of one head and
-// goes through the rows of the other side 64 at a time: a lane a row for the scores, a lane two elements for the sums.  Right for
-// every shape; bound by instruction issue and by rows that every wavefront reads again.
-#include "attention.h"
+// The gradient of attention over the caller's rows.  Probabilities are computed again from the scores and the logarithms of their
+// sums that the forward pass left, p = exp(s - lse); e = p (dp - delta) with dp = dout v and delta = dout out.  No atomics: every
+// result has one wavefront that sums it, in one order.
+//
+// Half precision: p enters its product times 2^12 (p <= 1, so it fits), which keeps the small probabilities of long rows out of the
+// type's subnormal numbers; dp and delta are taken times 2^-12 in exchange, where float32 loses nothing, so that e is what it is.
+#include "attention_mx.h"
 
 namespace ff {
 namespace {
 
-// p and e of one (query, key) pair of rows
-template <typename T>
-__device__ __forceinline__ void pair_terms(const Attn& a, int32_t rq, int32_t rk, int h, int kh, float* p, float* e) {
-  const T *q = row_of_head<T>(a.q, rq, h), *g = row_of_head<T>(a.dout, rq, h), *o = row_of_head<T>(a.out, rq, h);
-  const T *k = row_of_head<T>(a.k, rk, kh), *v = row_of_head<T>(a.v, rk, kh);
-  float s = 0.f, dp = 0.f, delta = 0.f;
-  for (int i = 0; i < a.D; ++i) {
-    const float gi = Elem<T>::load(g + i);
-    s = fmaf(Elem<T>::load(q + i), Elem<T>::load(k + i), s);
-    dp = fmaf(gi, Elem<T>::load(v + i), dp);
-    delta = fmaf(gi, Elem<T>::load(o + i), delta);
-  }
-  *p = expf(a.scale * s - a.lse[(int64_t)rq * a.H + h]);
-  *e = *p * (dp - delta) * a.scale;
+template <typename T> constexpr float kLift = 0.f;
+template <> constexpr float kLift<f16_t> = 12.f;
+template <typename T> constexpr float kLower = 1.f;
+template <> constexpr float kLower<f16_t> = 1.f / 4096.f;
+
+// The logarithm of a row's sum as the exponent's offset: base 2, and +infinity (every p zero) where the row has no key
+template <typename T> __device__ __forceinline__ float as_offset(float lse) {
+  return lse == -INFINITY ? INFINITY : lse * kLog2e - kLift<T>;
 }
 
-template <typename T> __global__ __launch_bounds__(64) void k_attention_dq_plain(Attn a) {
-  __shared__ float es[64];
-  __shared__ int32_t rows[64];
-  const int lane = threadIdx.x, h = blockIdx.y, kh = h / (a.H / a.K);
-  const int g = blockIdx.x / a.ql.G, i = blockIdx.x % a.ql.G;
-  if (g >= groups_of(a)) return;
-  const Span sq = span_of(a.ql, g), sk = span_of(a.kl, g);
-  if (i >= sq.len) return;
-  const int32_t row = row_at(a.ql, sq.at + i);
-  if (row < 0) return;
-  float d0 = 0.f, d1 = 0.f;
-  for (int j0 = 0; j0 < sk.len; j0 += 64) {
-    const int32_t r = j0 + lane < sk.len ? row_at(a.kl, sk.at + j0 + lane) : -1;
-    const bool ok = r >= 0 && (!a.mask || a.mask[r]);
-    float p = 0.f, e = 0.f;
-    if (ok) pair_terms<T>(a, row, r, h, kh, &p, &e);
-    es[lane] = e;
-    rows[lane] = ok ? r : -1;
-    __syncthreads();
-    for (int j = 0; j < 64; ++j) {
-      if (rows[j] < 0) continue;
-      const T* k = row_of_head<T>(a.k, rows[j], kh);
-      if (lane < a.D) d0 = fmaf(es[j], Elem<T>::load(k + lane), d0);
-      if (lane + 64 < a.D) d1 = fmaf(es[j], Elem<T>::load(k + lane + 64), d1);
+template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a, const Piece& b) {
+  float s = 0.f;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = fmaf(a.f[j], b.f[j], s);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      T x, y;
+      x.bits = (uint16_t)(a.q[j / 2] >> (16 * (j % 2)));
+      y.bits = (uint16_t)(b.q[j / 2] >> (16 * (j % 2)));
+      s = fmaf(Elem<T>::load(&x), Elem<T>::load(&y), s);
     }
-    __syncthreads();
   }
-  T* dq = row_of_head<T>(a.dq, row, h);
-  if (lane < a.D) Elem<T>::store(dq + lane, d0);
-  if (lane + 64 < a.D) Elem<T>::store(dq + lane + 64, d1);
+  return s;
 }
 
-template <typename T> __global__ __launch_bounds__(64) void k_attention_dkv_plain(Attn a) {
-  __shared__ float es[64], ps[64];
-  __shared__ int32_t rows[64];
-  const int lane = threadIdx.x, kh = blockIdx.y, share = a.H / a.K;
-  const int g = blockIdx.x / a.kl.G, i = blockIdx.x % a.kl.G;
-  if (g >= groups_of(a)) return;
-  const Span sq = span_of(a.ql, g), sk = span_of(a.kl, g);
-  if (i >= sk.len) return;
-  const int32_t row = row_at(a.kl, sk.at + i);
-  if (row < 0) return;
-  const bool ok = !a.mask || a.mask[row];
-  float k0 = 0.f, k1 = 0.f, v0 = 0.f, v1 = 0.f;
-  for (int h = kh * share; ok && h < (kh + 1) * share; ++h)
-    for (int j0 = 0; j0 < sq.len; j0 += 64) {
-      const int32_t r = j0 + lane < sq.len ? row_at(a.ql, sq.at + j0 + lane) : -1;
-      float p = 0.f, e = 0.f;
-      if (r >= 0) pair_terms<T>(a, r, row, h, kh, &p, &e);
-      es[lane] = e;
-      ps[lane] = p;
-      rows[lane] = r;
-      __syncthreads();
-      for (int j = 0; j < 64; ++j) {
-        if (rows[j] < 0) continue;
-        const T *q = row_of_head<T>(a.q, rows[j], h), *go = row_of_head<T>(a.dout, rows[j], h);
-        if (lane < a.D) {
-          k0 = fmaf(es[j], Elem<T>::load(q + lane), k0);
-          v0 = fmaf(ps[j], Elem<T>::load(go + lane), v0);
-        }
-        if (lane + 64 < a.D) {
-          k1 = fmaf(es[j], Elem<T>::load(q + lane + 64), k1);
-          v1 = fmaf(ps[j], Elem<T>::load(go + lane + 64), v1);
+// ---- short groups: a wavefront holds all keys, values and their gradients of a group and key head ---------------
+// Scores with the queries down and the keys across (Q K^T): a lane holds scores of one key, and p and e are the right operands of
+// (dv)^T = dout^T p and (dk)^T = q^T e as they lie in the registers.  For (dq)^T = K^T e^T e goes through LDS once, which turns it.
+// Queries by 32, delta from their own rows on the way.
+template <typename T, int DP, int KT>
+__global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool whole, bool whole_out) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, PQ = 2 / TILES;
+  constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 32 + PAD;
+  constexpr int PER = DP * (int)sizeof(T) / 16;
+  __shared__ __attribute__((aligned(16))) T keys_all[4][RK * (LD > LDE ? LD : LDE)];  // keys, then e
+  __shared__ __attribute__((aligned(16))) T rows_all[4][2][32 * LD];                  // q and dout
+  __shared__ __attribute__((aligned(16))) float stats_all[4][2][32];
+  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+  T *const et = keys_all[wave], *const qs = rows_all[wave][0], *const gs = rows_all[wave][1];
+  float *const offs = stats_all[wave][0], *const deltas = stats_all[wave][1];
+  const int share = a.H / a.K;
+  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
+  const int kh = (int)(item % a.K);
+  if (item / a.K >= groups_of(a)) return;
+  const int32_t group = (int32_t)(item / a.K);
+  const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
+  const int32_t rows = sq.len * share;
+
+  int32_t key[RK / 16];
+  uint32_t live = 0;  // bit t: key t of this lane is one that queries look at
+#pragma unroll
+  for (int t = 0; t < RK / 16; ++t) {
+    const int32_t p = t * 16 + i;
+    key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
+  }
+#pragma unroll
+  for (int t = 0; t < RK / 16; ++t)
+    if (key[t] >= 0 && (!a.mask || a.mask[key[t]])) live |= 1u << t;
+  Piece kf[KT][NF], vf[KT][NF];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      kf[t][f].q = vf[t][f].q = u32x4{0u, 0u, 0u, 0u};
+      if (live >> t & 1) {
+        kf[t][f] = load_piece(row_of_head<const T>(a.k, key[t], kh), f * KF + g4 * E, a.D, whole);
+        vf[t][f] = load_piece(row_of_head<const T>(a.v, key[t], kh), f * KF + g4 * E, a.D, whole);
+      }
+    }
+#pragma unroll
+  for (int t = 0; t < RK / 16; ++t)
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      if (f * 4 + g4 < PER) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LD + f * KF + g4 * E) = t < KT ? kf[t < KT ? t : 0][f].q : u32x4{0u, 0u, 0u, 0u};
+  wave_sync();
+  Piece kc[DT][KP];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int t = 0; t < KP; ++t) kc[d][t] = column_piece(et, LD, t * 16 * TILES, d * 16, lane);
+  wave_sync();
+  if constexpr (KT * 16 < RK) {  // e of the keys that make the last piece whole
+    for (int x = lane; x < (RK - KT * 16) * LDE / E; x += 64) *reinterpret_cast<u32x4*>(et + KT * 16 * LDE + x * E) = u32x4{0u, 0u, 0u, 0u};
+  }
+
+  const float c = a.scale * kLog2e;
+  f32x4 dk[KT][DT], dv[KT][DT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int32_t r0 = 0; r0 < rows; r0 += 32) {
+    QueryRow q[2];
+    Piece qf[2][NF], gf[2][NF];
+    float delta[2], off[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      q[u] = query_row(a, sq, share, kh, r0 + u * 16 + i);
+      delta[u] = 0.f;
+      off[u] = INFINITY;
+      if (q[u].row >= 0) off[u] = as_offset<T>(a.lse[(int64_t)q[u].row * a.H + q[u].h]);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        qf[u][f].q = gf[u][f].q = u32x4{0u, 0u, 0u, 0u};
+        if (q[u].row >= 0) {
+          qf[u][f] = load_piece(row_of_head<const T>(a.q, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
+          gf[u][f] = load_piece(row_of_head<const T>(a.dout, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
+          delta[u] += dot_pieces<T>(gf[u][f], load_piece(row_of_head<const T>(a.out, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole));
         }
       }
-      __syncthreads();
     }
-  T *dk = row_of_head<T>(a.dk, row, kh), *dv = row_of_head<T>(a.dv, row, kh);
-  if (lane < a.D) {
-    Elem<T>::store(dk + lane, k0);
-    Elem<T>::store(dv + lane, v0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      delta[u] = over_lanes16_sum(delta[u]) * kLower<T>;
+      if (g4 == 0) {
+        offs[u * 16 + i] = off[u];
+        deltas[u * 16 + i] = delta[u];
+      }
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        if (f * 4 + g4 < PER) {
+          *reinterpret_cast<u32x4*>(qs + (u * 16 + i) * LD + f * KF + g4 * E) = qf[u][f].q;
+          *reinterpret_cast<u32x4*>(gs + (u * 16 + i) * LD + f * KF + g4 * E) = gf[u][f].q;
+        }
+    }
+    wave_sync();
+    f32x4 fo[2], fd[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      fo[u] = *reinterpret_cast<const f32x4*>(offs + u * 16 + g4 * 4);
+      fd[u] = *reinterpret_cast<const f32x4*>(deltas + u * 16 + g4 * 4);
+    }
+    Piece qc[DT][PQ], gc[DT][PQ];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int u = 0; u < PQ; ++u) {
+        qc[d][u] = column_piece(qs, LD, u * 16 * TILES, d * 16, lane);
+        gc[d][u] = column_piece(gs, LD, u * 16 * TILES, d * 16, lane);
+      }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      f32x4 s[2], dp[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        s[u] = dp[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          s[u] = mma<T>(qf[u][f], kf[t][f], s[u]);
+          dp[u] = mma<T>(gf[u][f], vf[t][f], dp[u]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[u][r] = exp2_fast(fmaf(s[u][r], c, -fo[u][r]));
+          dp[u][r] = s[u][r] * fmaf(dp[u][r], kLower<T>, -fd[u][r]);
+        }
+      }
+      const bool here = live >> t & 1;
+      if (!__all(here)) {  // keys that no query looks at
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dp[u][r] = here ? dp[u][r] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < PQ; ++u) {
+        const Piece p = as_piece<T>(s + u * TILES), e = as_piece<T>(dp + u * TILES);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          dv[t][d] = mma<T>(gc[d][u], p, dv[t][d]);
+          dk[t][d] = mma<T>(qc[d][u], e, dk[t][d]);
+        }
+        if constexpr (sizeof(T) == 4) {
+          *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LDE + u * 16 + g4 * 4) = e.q;
+        } else {
+          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.s[0];
+          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + 16 + g4 * 4) = e.s[1];
+        }
+      }
+    }
+    wave_sync();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 dq[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) dq[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < KP; ++t) {
+        const Piece e = column_piece(et, LDE, t * 16 * TILES, u * 16, lane);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d] = mma<T>(kc[d][t], e, dq[d]);
+      }
+      if (q[u].row >= 0) {
+        T* to = row_of_head<T>(a.dq, q[u].row, q[u].h);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) store4(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D, whole_out);
+      }
+    }
+    wave_sync();
   }
-  if (lane + 64 < a.D) {
-    Elem<T>::store(dk + lane + 64, k1);
-    Elem<T>::store(dv + lane + 64, v1);
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    if (key[t] < 0) continue;
+    const bool here = live >> t & 1;
+    T *tk = row_of_head<T>(a.dk, key[t], kh), *tv = row_of_head<T>(a.dv, key[t], kh);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      store4(tk, d * 16 + g4 * 4, here ? dk[t][d] * a.scale : zero, a.D, whole_out);
+      store4(tv, d * 16 + g4 * 4, here ? dv[t][d] * kLower<T> : zero, a.D, whole_out);
+    }
   }
 }
 
-template <typename T> int backward(const Attn& a, hipStream_t stream) {
-  const int64_t sq = (int64_t)a.max_groups * a.ql.G, sk = (int64_t)a.max_groups * a.kl.G;
-  if (sq > INT32_MAX || sk > INT32_MAX || a.H > 65535) return FF_ERR_UNSUPPORTED;
-  k_attention_dq_plain<T><<<dim3((uint32_t)sq, a.H), 64, 0, stream>>>(a);
-  k_attention_dkv_plain<T><<<dim3((uint32_t)sk, a.K), 64, 0, stream>>>(a);
+// ---- any lengths -----------------------------------------------------------------------------------------
+// delta of every row and head: a few lanes a head, 16 bytes each
+template <typename T, int DP> __global__ __launch_bounds__(256) void k_attention_delta(Attn a, bool whole) {
+  constexpr int PER = DP * (int)sizeof(T) / 16;
+  const int64_t x = (int64_t)blockIdx.x * (256 / PER) + threadIdx.x / PER, all = (int64_t)a.ql.n * a.H;
+  const int e = (threadIdx.x % PER) * Mx<T>::E;
+  float s = 0.f;
+  if (x < all) {
+    const int32_t row = (int32_t)(x / a.H), h = (int32_t)(x % a.H);
+    s = dot_pieces<T>(load_piece(row_of_head<const T>(a.dout, row, h), e, a.D, whole), load_piece(row_of_head<const T>(a.out, row, h), e, a.D, whole));
+  }
+#pragma unroll
+  for (int d = PER / 2; d; d >>= 1) s += __shfl_xor(s, d);
+  if (x < all && threadIdx.x % PER == 0) a.delta[x] = s;
+}
+
+// dk and dv: NW wavefronts of KW x 16 keys each hold keys, values and the sums of their gradients; the queries that look at them and
+// the gradients of their results go by in tiles of 32 rows through LDS.  splits > 1: each workgroup takes a stretch of the queries.
+template <typename T, int DP, int NW, int KW>
+__global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, int splits, float* part, bool whole, bool whole_out) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW, BQ = 32, PQ = 2 / TILES;
+  constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T);
+  typedef Rows<T, DP, BQ, NT> R;
+  __shared__ __attribute__((aligned(16))) T qs[2][BQ * LD];
+  __shared__ __attribute__((aligned(16))) T gs[2][BQ * LD];
+  __shared__ __attribute__((aligned(16))) float offs[2][BQ], deltas[2][BQ];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15, share = a.H / a.K;
+  const int split = blockIdx.x % splits;
+  const int32_t rest = blockIdx.x / splits;
+  const int kh = rest / tg.tiles;
+  const TileAt at = tile_at<16 * NW * KW>(a, a.kl, tg, rest - kh * tg.tiles, lane);
+  if (at.g < 0) return;
+  const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
+  const int32_t k0 = at.tile * (16 * NW * KW);
+  if (at.tile > sk.len / (16 * NW * KW) || k0 >= sk.len) return;
+  const int32_t all_rows = sq.len * share, tiles = (all_rows + BQ - 1) / BQ, per = (tiles + splits - 1) / splits;
+  const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+
+  int32_t rows[R::U], heads[R::U];
+  auto number = [&](int32_t t) {
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      const int r = R::row(tid, u);
+      QueryRow q = {-1, 0};
+      if (t < t1 && r < BQ) q = query_row(a, sq, share, kh, t * BQ + r);
+      rows[u] = q.row;
+      heads[u] = q.h;
+    }
+  };
+  Piece qr[R::U], gr[R::U];
+  float fo[R::U], fd[R::U];
+  auto fetch = [&]() {
+    R::fetch(qr, a.q, rows, heads, tid, a.D, whole);
+    R::fetch(gr, a.dout, rows, heads, tid, a.D, whole);
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      fo[u] = INFINITY;
+      fd[u] = 0.f;
+      if (tid % R::PER == 0 && rows[u] >= 0) {
+        fo[u] = as_offset<T>(a.lse[(int64_t)rows[u] * a.H + heads[u]]);
+        fd[u] = a.delta[(int64_t)rows[u] * a.H + heads[u]] * kLower<T>;
+      }
+    }
+  };
+  number(t0);
+  int32_t key[KW];
+  bool live[KW];
+#pragma unroll
+  for (int t = 0; t < KW; ++t) {
+    const int32_t p = k0 + (wave * KW + t) * 16 + i;
+    key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
+    live[t] = key[t] >= 0 && (!a.mask || a.mask[key[t]]);
+  }
+  fetch();
+  number(t0 + 1);
+  Piece kf[KW][NF], vf[KW][NF];
+#pragma unroll
+  for (int t = 0; t < KW; ++t)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      kf[t][f].q = vf[t][f].q = u32x4{0u, 0u, 0u, 0u};
+      if (live[t]) {
+        kf[t][f] = load_piece(row_of_head<const T>(a.k, key[t], kh), f * KF + g4 * E, a.D, whole);
+        vf[t][f] = load_piece(row_of_head<const T>(a.v, key[t], kh), f * KF + g4 * E, a.D, whole);
+      }
+    }
+  if constexpr (W > DP) {
+    for (int x = tid; x < 2 * BQ; x += NT)
+#pragma unroll
+      for (int e = DP; e < W; e += E) {
+        *reinterpret_cast<u32x4*>(&qs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4*>(&gs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
+      }
+  }
+  const float c = a.scale * kLog2e;
+  f32x4 dk[KW][DT], dv[KW][DT];
+#pragma unroll
+  for (int t = 0; t < KW; ++t)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int32_t t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    R::put(qs[buf], LD, qr, tid);
+    R::put(gs[buf], LD, gr, tid);
+    if (tid % R::PER == 0) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u)
+        if (BQ * R::PER % NT == 0 || R::row(tid, u) < BQ) {
+          offs[buf][R::row(tid, u)] = fo[u];
+          deltas[buf][R::row(tid, u)] = fd[u];
+        }
+    }
+    __syncthreads();
+    if (t + 1 < t1) {
+      fetch();
+      number(t + 2);
+    }
+    f32x4 s[KW][2], dp[KW][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int k = 0; k < KW; ++k) s[k][u] = dp[k][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const Piece qf = row_piece(qs[buf], LD, u * 16 + i, f * KF + g4 * E), gf = row_piece(gs[buf], LD, u * 16 + i, f * KF + g4 * E);
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+          s[k][u] = mma<T>(qf, kf[k][f], s[k][u]);
+          dp[k][u] = mma<T>(gf, vf[k][f], dp[k][u]);
+        }
+      }
+      const f32x4 o = *reinterpret_cast<const f32x4*>(offs[buf] + u * 16 + g4 * 4), l = *reinterpret_cast<const f32x4*>(deltas[buf] + u * 16 + g4 * 4);
+#pragma unroll
+      for (int k = 0; k < KW; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[k][u][r] = exp2_fast(fmaf(s[k][u][r], c, -o[r]));
+          dp[k][u][r] = s[k][u][r] * fmaf(dp[k][u][r], kLower<T>, -l[r]);
+        }
+    }
+    Piece p[KW][PQ], e[KW][PQ];
+#pragma unroll
+    for (int k = 0; k < KW; ++k)
+#pragma unroll
+      for (int u = 0; u < PQ; ++u) {
+        p[k][u] = as_piece<T>(s[k] + u * TILES);
+        e[k][u] = as_piece<T>(dp[k] + u * TILES);
+      }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int u = 0; u < PQ; ++u) {
+        const Piece gc = column_piece(gs[buf], LD, u * 16 * TILES, d * 16, lane), qc = column_piece(qs[buf], LD, u * 16 * TILES, d * 16, lane);
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+          dv[k][d] = mma<T>(gc, p[k][u], dv[k][d]);
+          dk[k][d] = mma<T>(qc, e[k][u], dk[k][d]);
+        }
+      }
+  }
+#pragma unroll
+  for (int t = 0; t < KW; ++t) {
+    if (key[t] < 0) continue;
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (splits > 1) {
+      const int64_t all = (int64_t)a.kl.n * a.K;
+      float* to = part + (split * all + (int64_t)key[t] * a.K + kh) * 2 * DP + g4 * 4;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        *reinterpret_cast<f32x4*>(to + d * 16) = live[t] ? dk[t][d] : zero;
+        *reinterpret_cast<f32x4*>(to + DP + d * 16) = live[t] ? dv[t][d] : zero;
+      }
+      continue;
+    }
+    T *tk = row_of_head<T>(a.dk, key[t], kh), *tv = row_of_head<T>(a.dv, key[t], kh);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      store4(tk, d * 16 + g4 * 4, live[t] ? dk[t][d] * a.scale : zero, a.D, whole_out);
+      store4(tv, d * 16 + g4 * 4, live[t] ? dv[t][d] * kLower<T> : zero, a.D, whole_out);
+    }
+  }
+}
+
+// dq: the forward kernel's arrangement, with keys and values by BK through LDS and scores with the keys down (K Q^T), so that e is the
+// right operand of (dq)^T = K^T e^T as it lies in the registers.
+template <typename T, int DP, int NW, int QT, int BK>
+__global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, int splits, float* part, bool whole, bool whole_out) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
+  constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T), BQ = 16 * QT * NW;
+  typedef Rows<T, DP, BK, NT> R;
+  __shared__ __attribute__((aligned(16))) T ks[2][BK * LD];
+  __shared__ __attribute__((aligned(16))) T vs[2][BK * LD];
+  __shared__ __attribute__((aligned(16))) float bias[2][BK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
+  const int split = blockIdx.x % splits;
+  const int32_t rest = blockIdx.x / splits;
+  const int kh = rest / tg.tiles;
+  const TileAt at = tile_at<BQ>(a, a.ql, tg, rest - kh * tg.tiles, lane);
+  if (at.g < 0) return;
+  const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
+  if ((int64_t)at.tile * BQ >= (int64_t)sq.len * tg.share) return;
+  const int32_t tiles = (sk.len + BK - 1) / BK, per = (tiles + splits - 1) / splits;
+  const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+
+  int32_t rows[R::U], heads[R::U];
+  auto number = [&](int32_t t) {
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      const int r = R::row(tid, u);
+      const int32_t p = t * BK + r;
+      rows[u] = t < t1 && r < BK && p < sk.len ? row_at(a.kl, sk.at + p) : -1;
+      heads[u] = kh;
+      if (a.mask && rows[u] >= 0 && !a.mask[rows[u]]) rows[u] = -1;
+    }
+  };
+  Piece kr[R::U], vr[R::U];
+  float br[R::U];
+  auto fetch = [&]() {
+    R::fetch(kr, a.k, rows, heads, tid, a.D, whole);
+    R::fetch(vr, a.v, rows, heads, tid, a.D, whole);
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) br[u] = rows[u] >= 0 ? 0.f : -INFINITY;
+  };
+  number(t0);
+  QueryRow q[QT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
+  fetch();
+  number(t0 + 1);
+  Piece qf[QT][NF], gf[QT][NF];
+  float off[QT], delta[QT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    off[u] = INFINITY;
+    delta[u] = 0.f;
+    if (q[u].row >= 0) {
+      off[u] = as_offset<T>(a.lse[(int64_t)q[u].row * a.H + q[u].h]);
+      delta[u] = a.delta[(int64_t)q[u].row * a.H + q[u].h] * kLower<T>;
+    }
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      qf[u][f].q = gf[u][f].q = u32x4{0u, 0u, 0u, 0u};
+      if (q[u].row >= 0) {
+        qf[u][f] = load_piece(row_of_head<const T>(a.q, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
+        gf[u][f] = load_piece(row_of_head<const T>(a.dout, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
+      }
+    }
+  }
+  if constexpr (W > DP) {
+    for (int x = tid; x < 2 * BK; x += NT)
+#pragma unroll
+      for (int e = DP; e < W; e += E) {
+        *reinterpret_cast<u32x4*>(&ks[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4*>(&vs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
+      }
+  }
+  const float c = a.scale * kLog2e;
+  f32x4 dq[QT][DT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u)
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dq[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int32_t t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    R::put(ks[buf], LD, kr, tid);
+    R::put(vs[buf], LD, vr, tid);
+    if (tid % R::PER == 0) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u)
+        if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[buf][R::row(tid, u)] = br[u];
+    }
+    __syncthreads();
+    if (t + 1 < t1) {
+      fetch();
+      number(t + 2);
+    }
+#pragma unroll
+    for (int k = 0; k < BK / 16 / TILES; ++k) {
+      f32x4 s[QT][TILES], dp[QT][TILES];
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        const int r = (k * TILES + x) * 16;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) s[u][x] = dp[u][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const Piece kf = row_piece(ks[buf], LD, r + i, f * KF + g4 * E), vf = row_piece(vs[buf], LD, r + i, f * KF + g4 * E);
+#pragma unroll
+          for (int u = 0; u < QT; ++u) {
+            s[u][x] = mma<T>(kf, qf[u][f], s[u][x]);
+            dp[u][x] = mma<T>(vf, gf[u][f], dp[u][x]);
+          }
+        }
+        const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + r + g4 * 4);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = exp2_fast(fmaf(s[u][x][j], c, b[j]) - off[u]);
+            dp[u][x][j] = p * fmaf(dp[u][x][j], kLower<T>, -delta[u]);
+          }
+      }
+      Piece e[QT];
+#pragma unroll
+      for (int u = 0; u < QT; ++u) e[u] = as_piece<T>(dp[u]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const Piece kc = column_piece(ks[buf], LD, k * 16 * TILES, d * 16, lane);
+#pragma unroll
+        for (int u = 0; u < QT; ++u) dq[u][d] = mma<T>(kc, e[u], dq[u][d]);
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    if (q[u].row < 0) continue;
+    if (splits > 1) {
+      const int64_t all = (int64_t)a.ql.n * a.H;
+      float* to = part + (split * all + (int64_t)q[u].row * a.H + q[u].h) * DP + g4 * 4;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(to + d * 16) = dq[u][d];
+      continue;
+    }
+    T* to = row_of_head<T>(a.dq, q[u].row, q[u].h);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) store4(to, d * 16 + g4 * 4, dq[u][d] * a.scale, a.D, whole_out);
+  }
+}
+
+// Sums of the stretches, a wavefront a row and head; N arrays of DP sums lie side by side in a part.
+template <typename T, int DP, int N>
+__global__ __launch_bounds__(256) void k_attention_sum(Attn a, GroupList l, TileGrid tg, int heads, int splits, const float* part, Heads to0, Heads to1,
+                                                       float by0, float by1) {
+  const int lane = threadIdx.x & 63;
+  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int h = (int)(x / tg.tiles);
+  if (h >= heads) return;
+  const TileAt at = tile_at<1>(a, l, tg, (int32_t)(x - (int64_t)h * tg.tiles), lane);
+  if (at.g < 0) return;
+  const Span sp = span_of(l, at.g);
+  const int32_t row = at.tile < sp.len ? row_at(l, sp.at + at.tile) : -1;
+  if (row < 0) return;
+  const int64_t all = (int64_t)l.n * heads * N * DP;
+  part += ((int64_t)row * heads + h) * N * DP;
+  for (int e = lane; e < N * DP; e += 64) {
+    float s = 0.f;
+    for (int k = 0; k < splits; ++k) s += part[k * all + e];
+    const int d = e % DP;
+    if (d < a.D) Elem<T>::store(row_of_head<T>(e < DP ? to0 : to1, row, h) + d, s * (e < DP ? by0 : by1));
+  }
+}
+
+// ---- which kernels -----------------------------------------------------------------------------------------
+struct Plan {
+  bool group;
+  bool wide_q, wide_k;  // dq: four wavefronts of 32 rows, else one of 16; dkv: four of 32 keys, else one of 16
+  TileGrid tq, tk, sum_q, sum_k;
+  int splits_q, splits_k;
+  bool fits;
+  size_t delta, parts_q, parts_k, bytes;  // of the workspace: delta, then the parts of dq, then those of dk and dv
+};
+// Stretches of the other side's rows, so that few tiles fill the chip; 256 rows a stretch at least
+int stretches(int64_t groups, int waves, int64_t other) {
+  if (groups < 1 || groups * waves * 2 > kChipWaves) return 1;
+  const int64_t s = ceil_div(kChipWaves, groups * waves), most = other / 256 > 0 ? other / 256 : 1;
+  return (int)(s < most ? s : most);
+}
+Plan plan(const Attn& a, size_t size) {
+  Plan p{};
+  const int DP = padded(a.D), share = a.H / a.K;
+  const int64_t rows = (int64_t)a.ql.G * share;
+  p.fits = true;
+  p.group = a.kl.G <= 128 && DP <= 32 && rows <= 512;
+  (void)size;
+  if (p.group) {
+    p.fits = ceil_div((int64_t)a.max_groups * a.K, 4) <= INT32_MAX;
+    return p;
+  }
+  bool f[4];
+  p.wide_q = rows > 32;
+  p.wide_k = a.kl.G > 32;
+  p.tq = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, p.wide_q ? 128 : 16, &f[0]);
+  p.tk = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, p.wide_k ? 128 : 16, &f[1]);
+  p.sum_q = tile_grid(a.ql.n, a.ql.G, 1, a.max_groups, 1, &f[2]);
+  p.sum_k = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, 1, &f[3]);
+  const int64_t gq = (int64_t)p.tq.tiles * a.K, gk = (int64_t)p.tk.tiles * a.K;
+  p.splits_q = stretches(gq, p.wide_q ? 4 : 1, a.kl.G);
+  p.splits_k = stretches(gk, p.wide_k ? 4 : 1, rows);
+  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX && gk * p.splits_k <= INT32_MAX && ceil_div((int64_t)a.ql.n * a.H, 8) <= INT32_MAX &&
+           rows <= INT32_MAX - 64;
+  if (p.splits_q > 1) p.fits = p.fits && f[2] && (int64_t)p.sum_q.tiles * a.H <= INT32_MAX;
+  if (p.splits_k > 1) p.fits = p.fits && f[3] && (int64_t)p.sum_k.tiles * a.K <= INT32_MAX;
+  p.delta = align_up((size_t)a.ql.n * a.H * 4, 256);
+  p.parts_q = p.splits_q > 1 ? align_up((size_t)p.splits_q * a.ql.n * a.H * DP * 4, 256) : 0;
+  p.parts_k = p.splits_k > 1 ? align_up((size_t)p.splits_k * a.kl.n * a.K * DP * 8, 256) : 0;
+  p.bytes = p.delta + p.parts_q + p.parts_k;
+  return p;
+}
+
+template <typename T, int DP, int KT> int group_launch(const Attn& a, bool whole, bool whole_out, hipStream_t st) {
+  k_attention_backward_group<T, DP, KT><<<dim3((uint32_t)ceil_div((int64_t)a.max_groups * a.K, 4)), 256, 0, st>>>(a, whole, whole_out);
   return launch_status();
+}
+template <typename T, int DP> int run(Attn a, const Plan& p, char* ws, hipStream_t st) {
+  bool whole = true, whole_out = true;
+  for (const Heads* x : {&a.q, &a.k, &a.v, &a.out, &a.dout}) whole = whole && whole_pieces(*x, a.D, sizeof(T));
+  for (const Heads* x : {&a.dq, &a.dk, &a.dv}) whole_out = whole_out && whole_pieces(*x, a.D, sizeof(T));
+  if constexpr (DP <= 32) {
+    if (p.group) {
+      const int kt = (a.kl.G + 15) / 16;
+      if (kt <= 2) return group_launch<T, DP, 2>(a, whole, whole_out, st);
+      if (kt <= 4) return group_launch<T, DP, 4>(a, whole, whole_out, st);
+      if (kt <= 5) return group_launch<T, DP, 5>(a, whole, whole_out, st);
+      if (kt <= 6) return group_launch<T, DP, 6>(a, whole, whole_out, st);
+      return group_launch<T, DP, 8>(a, whole, whole_out, st);
+    }
+  }
+  a.delta = reinterpret_cast<float*>(ws);
+  float *pq = reinterpret_cast<float*>(ws + p.delta), *pk = reinterpret_cast<float*>(ws + p.delta + p.parts_q);
+  if (a.ql.n > 0) {
+    constexpr int PER = DP * (int)sizeof(T) / 16;
+    k_attention_delta<T, DP><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a, whole);
+    const dim3 grid((uint32_t)((int64_t)p.tq.tiles * a.K * p.splits_q));
+    if (p.wide_q)
+      k_attention_dq<T, DP, 4, 2, 32><<<grid, 256, 0, st>>>(a, p.tq, p.splits_q, pq, whole, whole_out);
+    else
+      k_attention_dq<T, DP, 1, 1, 32><<<grid, 64, 0, st>>>(a, p.tq, p.splits_q, pq, whole, whole_out);
+    if (p.splits_q > 1)
+      k_attention_sum<T, DP, 1><<<dim3((uint32_t)ceil_div((int64_t)p.sum_q.tiles * a.H, 4)), 256, 0, st>>>(a, a.ql, p.sum_q, a.H, p.splits_q, pq, a.dq,
+                                                                                                       a.dq, a.scale, a.scale);
+  }
+  if (a.kl.n > 0) {
+    const dim3 grid((uint32_t)((int64_t)p.tk.tiles * a.K * p.splits_k));
+    if (p.wide_k)
+      k_attention_dkv<T, DP, 4, 2><<<grid, 256, 0, st>>>(a, p.tk, p.splits_k, pk, whole, whole_out);
+    else
+      k_attention_dkv<T, DP, 1, 1><<<grid, 64, 0, st>>>(a, p.tk, p.splits_k, pk, whole, whole_out);
+    if (p.splits_k > 1)
+      k_attention_sum<T, DP, 2><<<dim3((uint32_t)ceil_div((int64_t)p.sum_k.tiles * a.K, 4)), 256, 0, st>>>(a, a.kl, p.sum_k, a.K, p.splits_k, pk, a.dk,
+                                                                                                       a.dv, a.scale, kLower<T>);
+  }
+  return launch_status();
+}
+template <typename T> int run_type(const Attn& a, const Plan& p, char* ws, hipStream_t st) {
+  switch (padded(a.D)) {
+    case 16: return run<T, 16>(a, p, ws, st);
+    case 32: return run<T, 32>(a, p, ws, st);
+    case 64: return run<T, 64>(a, p, ws, st);
+    default: return run<T, 128>(a, p, ws, st);
+  }
 }
 
 }  // namespace
 
-size_t attention_backward_workspace_bytes(const Attn&, int) { return 0; }
-int attention_backward_launch(const Attn& a, int dtype, void*, hipStream_t stream) {
-  return dtype == FF_F32 ? backward<float>(a, stream) : dtype == FF_BF16 ? backward<bf16_t>(a, stream) : backward<f16_t>(a, stream);
+size_t attention_backward_workspace_bytes(const Attn& a, int dtype) { return plan(a, dtype == FF_F32 ? 4 : 2).bytes; }
+
+int attention_backward_launch(const Attn& a, int dtype, void* workspace, hipStream_t stream) {
+  const Plan p = plan(a, dtype == FF_F32 ? 4 : 2);
+  if (!p.fits) return FF_ERR_UNSUPPORTED;
+  char* ws = reinterpret_cast<char*>(workspace);
+  return dtype == FF_F32    ? run_type<float>(a, p, ws, stream)
+         : dtype == FF_BF16 ? run_type<bf16_t>(a, p, ws, stream)
+                            : run_type<f16_t>(a, p, ws, stream);
 }
 
 }  // namespace ff

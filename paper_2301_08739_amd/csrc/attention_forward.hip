@@ -6,15 +6,6 @@
 namespace ff {
 namespace {
 
-// A row of queries among those of a group that share their keys: row v is position v / share, head v % share of the key head's
-struct QueryRow {
-  int32_t row, h;  // row < 0: none
-};
-__device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int share, int kh, int32_t v) {
-  const int32_t p = share == 1 ? v : v / share, h = kh * share + (share == 1 ? 0 : v - p * share);
-  return {p < sq.len ? row_at(a.ql, sq.at + p) : -1, h};
-}
-
 // ---- short groups: a wavefront holds all keys and values of a group and head ----------------------------------
 // Keys and values are read once into registers (values through LDS, which turns them), the queries go by 16 at a time.
 template <typename T, int DP, int KT>
@@ -347,10 +338,6 @@ __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int
 }
 
 // ---- which kernel ---------------------------------------------------------------------------------------
-constexpr int kChipWaves = 2048;  // two wavefronts a SIMD
-
-int padded(int D) { return D <= 16 ? 16 : D <= 32 ? 32 : D <= 64 ? 64 : 128; }
-
 struct Plan {
   bool group;       // k_attention_group
   int parts;        // of a group's queries there

@@ -209,10 +209,23 @@ template <typename T, int DP, int R, int NT> struct Rows {
   }
 };
 
+// A row of queries among those of a group that share their keys: row v is position v / share, head v % share of the key head's
+struct QueryRow {
+  int32_t row, h;  // row < 0: none
+};
+__device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int share, int kh, int32_t v) {
+  const int32_t p = share == 1 ? v : v / share, h = kh * share + (share == 1 ? 0 : v - p * share);
+  return {p < sq.len ? row_at(a.ql, sq.at + p) : -1, h};
+}
+
 // May rows of this array be read and written in pieces of 16 bytes?
 inline bool whole_pieces(const Heads& x, int D, size_t size) {
   return ((uintptr_t)x.p | (uintptr_t)(x.rs * size) | (uintptr_t)(x.hs * size) | (uintptr_t)(D * size)) % 16 == 0;
 }
+
+constexpr int kChipWaves = 2048;  // two wavefronts a SIMD
+
+inline int padded(int D) { return D <= 16 ? 16 : D <= 32 ? 32 : D <= 64 ? 64 : 128; }
 
 }  // namespace
 }  // namespace ff

@@ -93,8 +93,18 @@ def test_rows_that_share_elements(lib):
     packed = dict(dq=_heads("dq", H, at=at, rs=width), dk=_heads("dk", K, at=at + 2 * H * D, rs=width), dv=_heads("dv", K, at=at + 2 * (H + K) * D, rs=width))
     meets = dict(packed, dk=_heads("dk", K, at=at + 2 * H * D - 2, rs=width))
     assert _backward(lib, s, **meets) == ARG
+    few = _shape(nq=2, nk=1 << 20, G=1, key_G=1 << 20, max_groups=2)
+    assert _backward(lib, few, **packed, ws=(at, 1 << 40)) == ARG                        # the workspace in the gradients
     assert _backward(lib, s, dq=_heads("dq", H, at=AT["perm"])) == ARG
     assert _forward(lib, s, out=_heads("out", H, at=AT["off"])) == ARG
+
+
+def test_workspaces(lib):
+    few = _shape(nq=2, nk=1 << 20, G=1, key_G=1 << 20, max_groups=2)
+    for run, need in ((_forward, lib.ff_attention_workspace_bytes(few, 1)), (_backward, lib.ff_attention_backward_workspace_bytes(few, 1))):
+        assert need > 0
+        for ws in ((None, 0), (AT["ws"], need - 1), (AT["ws"] + 128, need)):
+            assert run(lib, few, ws=ws) == WORKSPACE
 
 
 def test_empty_calls_launch_nothing(lib):
