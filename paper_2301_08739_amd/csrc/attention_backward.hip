@@ -40,8 +40,8 @@ template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a
 // Scores with the queries down and the keys across (Q K^T): a lane holds scores of one key, and p and e are the right operands of
 // (dv)^T = dout^T p and (dk)^T = q^T e as they lie in the registers.  For (dq)^T = K^T e^T e goes through LDS once, which turns it.
 // Queries by 32, delta from their own rows on the way.
-template <typename T, int DP, int KT>
-__global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool whole, bool whole_out) {
+template <typename T, int DP, int KT, bool WHOLE>
+__global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1) void k_attention_backward_group(Attn a) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, PQ = 2 / TILES;
   constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 32 + PAD;
   constexpr int PER = DP * (int)sizeof(T) / 16;
@@ -74,11 +74,8 @@ __global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool w
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      kf[t][f].q = vf[t][f].q = u32x4{0u, 0u, 0u, 0u};
-      if (live >> t & 1) {
-        kf[t][f] = load_piece(row_of_head<const T>(a.k, key[t], kh), f * KF + g4 * E, a.D, whole);
-        vf[t][f] = load_piece(row_of_head<const T>(a.v, key[t], kh), f * KF + g4 * E, a.D, whole);
-      }
+      kf[t][f] = load_piece<T, WHOLE>(a.k, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
+      vf[t][f] = load_piece<T, WHOLE>(a.v, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
     }
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t)
@@ -115,12 +112,9 @@ __global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool w
       if (q[u].row >= 0) off[u] = as_offset<T>(a.lse[(int64_t)q[u].row * a.H + q[u].h]);
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
-        qf[u][f].q = gf[u][f].q = u32x4{0u, 0u, 0u, 0u};
-        if (q[u].row >= 0) {
-          qf[u][f] = load_piece(row_of_head<const T>(a.q, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
-          gf[u][f] = load_piece(row_of_head<const T>(a.dout, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
-          delta[u] += dot_pieces<T>(gf[u][f], load_piece(row_of_head<const T>(a.out, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole));
-        }
+        qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
+        gf[u][f] = load_piece<T, WHOLE>(a.dout, q[u].row, q[u].h, f * KF + g4 * E, a.D);
+        delta[u] += dot_pieces<T>(gf[u][f], load_piece<T, WHOLE>(a.out, q[u].row, q[u].h, f * KF + g4 * E, a.D));
       }
     }
 #pragma unroll
@@ -207,7 +201,7 @@ __global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool w
       if (q[u].row >= 0) {
         T* to = row_of_head<T>(a.dq, q[u].row, q[u].h);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) store4(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D, whole_out);
+        for (int d = 0; d < DT; ++d) store4<T, WHOLE>(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D);
       }
     }
     wave_sync();
@@ -220,22 +214,22 @@ __global__ __launch_bounds__(256) void k_attention_backward_group(Attn a, bool w
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      store4(tk, d * 16 + g4 * 4, here ? dk[t][d] * a.scale : zero, a.D, whole_out);
-      store4(tv, d * 16 + g4 * 4, here ? dv[t][d] * kLower<T> : zero, a.D, whole_out);
+      store4<T, WHOLE>(tk, d * 16 + g4 * 4, here ? dk[t][d] * a.scale : zero, a.D);
+      store4<T, WHOLE>(tv, d * 16 + g4 * 4, here ? dv[t][d] * kLower<T> : zero, a.D);
     }
   }
 }
 
 // ---- any lengths -----------------------------------------------------------------------------------------
 // delta of every row and head: a few lanes a head, 16 bytes each
-template <typename T, int DP> __global__ __launch_bounds__(256) void k_attention_delta(Attn a, bool whole) {
+template <typename T, int DP, bool WHOLE> __global__ __launch_bounds__(256) void k_attention_delta(Attn a) {
   constexpr int PER = DP * (int)sizeof(T) / 16;
   const int64_t x = (int64_t)blockIdx.x * (256 / PER) + threadIdx.x / PER, all = (int64_t)a.ql.n * a.H;
   const int e = (threadIdx.x % PER) * Mx<T>::E;
   float s = 0.f;
   if (x < all) {
     const int32_t row = (int32_t)(x / a.H), h = (int32_t)(x % a.H);
-    s = dot_pieces<T>(load_piece(row_of_head<const T>(a.dout, row, h), e, a.D, whole), load_piece(row_of_head<const T>(a.out, row, h), e, a.D, whole));
+    s = dot_pieces<T>(load_piece<T, WHOLE>(a.dout, row, h, e, a.D), load_piece<T, WHOLE>(a.out, row, h, e, a.D));
   }
 #pragma unroll
   for (int d = PER / 2; d; d >>= 1) s += __shfl_xor(s, d);
@@ -244,14 +238,15 @@ template <typename T, int DP> __global__ __launch_bounds__(256) void k_attention
 
 // dk and dv: NW wavefronts of KW x 16 keys each hold keys, values and the sums of their gradients; the queries that look at them and
 // the gradients of their results go by in tiles of 32 rows through LDS.  splits > 1: each workgroup takes a stretch of the queries.
-template <typename T, int DP, int NW, int KW>
-__global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, int splits, float* part, bool whole, bool whole_out) {
+template <typename T, int DP, int NW, int KW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_attention_dkv(Attn a, TileGrid tg, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW, BQ = 32, PQ = 2 / TILES;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T);
   typedef Rows<T, DP, BQ, NT> R;
-  __shared__ __attribute__((aligned(16))) T qs[2][BQ * LD];
-  __shared__ __attribute__((aligned(16))) T gs[2][BQ * LD];
-  __shared__ __attribute__((aligned(16))) float offs[2][BQ], deltas[2][BQ];
+  constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
+  __shared__ __attribute__((aligned(16))) T qs[NB][BQ * LD];
+  __shared__ __attribute__((aligned(16))) T gs[NB][BQ * LD];
+  __shared__ __attribute__((aligned(16))) float offs[NB][BQ], deltas[NB][BQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15, share = a.H / a.K;
   const int split = blockIdx.x % splits;
   const int32_t rest = blockIdx.x / splits;
@@ -278,8 +273,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, 
   Piece qr[R::U], gr[R::U];
   float fo[R::U], fd[R::U];
   auto fetch = [&]() {
-    R::fetch(qr, a.q, rows, heads, tid, a.D, whole);
-    R::fetch(gr, a.dout, rows, heads, tid, a.D, whole);
+    R::template fetch<WHOLE>(qr, a.q, rows, heads, tid, a.D);
+    R::template fetch<WHOLE>(gr, a.dout, rows, heads, tid, a.D);
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
       fo[u] = INFINITY;
@@ -306,14 +301,11 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, 
   for (int t = 0; t < KW; ++t)
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      kf[t][f].q = vf[t][f].q = u32x4{0u, 0u, 0u, 0u};
-      if (live[t]) {
-        kf[t][f] = load_piece(row_of_head<const T>(a.k, key[t], kh), f * KF + g4 * E, a.D, whole);
-        vf[t][f] = load_piece(row_of_head<const T>(a.v, key[t], kh), f * KF + g4 * E, a.D, whole);
-      }
+      kf[t][f] = load_piece<T, WHOLE>(a.k, live[t] ? key[t] : -1, kh, f * KF + g4 * E, a.D);
+      vf[t][f] = load_piece<T, WHOLE>(a.v, live[t] ? key[t] : -1, kh, f * KF + g4 * E, a.D);
     }
   if constexpr (W > DP) {
-    for (int x = tid; x < 2 * BQ; x += NT)
+    for (int x = tid; x < NB * BQ; x += NT)
 #pragma unroll
       for (int e = DP; e < W; e += E) {
         *reinterpret_cast<u32x4*>(&qs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
@@ -327,7 +319,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, 
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int32_t t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+    const int buf = NB == 1 ? 0 : (t - t0) & 1;
+    if constexpr (NB == 1) wave_sync();
     R::put(qs[buf], LD, qr, tid);
     R::put(gs[buf], LD, gr, tid);
     if (tid % R::PER == 0) {
@@ -338,7 +331,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, 
           deltas[buf][R::row(tid, u)] = fd[u];
         }
     }
-    __syncthreads();
+    if constexpr (NB == 1) wave_sync();
+    else __syncthreads();
     if (t + 1 < t1) {
       fetch();
       number(t + 2);
@@ -403,22 +397,23 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dkv(Attn a, TileGrid tg, 
     T *tk = row_of_head<T>(a.dk, key[t], kh), *tv = row_of_head<T>(a.dv, key[t], kh);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      store4(tk, d * 16 + g4 * 4, live[t] ? dk[t][d] * a.scale : zero, a.D, whole_out);
-      store4(tv, d * 16 + g4 * 4, live[t] ? dv[t][d] * kLower<T> : zero, a.D, whole_out);
+      store4<T, WHOLE>(tk, d * 16 + g4 * 4, live[t] ? dk[t][d] * a.scale : zero, a.D);
+      store4<T, WHOLE>(tv, d * 16 + g4 * 4, live[t] ? dv[t][d] * kLower<T> : zero, a.D);
     }
   }
 }
 
 // dq: the forward kernel's arrangement, with keys and values by BK through LDS and scores with the keys down (K Q^T), so that e is the
 // right operand of (dq)^T = K^T e^T as it lies in the registers.
-template <typename T, int DP, int NW, int QT, int BK>
-__global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, int splits, float* part, bool whole, bool whole_out) {
+template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(Attn a, TileGrid tg, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T), BQ = 16 * QT * NW;
   typedef Rows<T, DP, BK, NT> R;
-  __shared__ __attribute__((aligned(16))) T ks[2][BK * LD];
-  __shared__ __attribute__((aligned(16))) T vs[2][BK * LD];
-  __shared__ __attribute__((aligned(16))) float bias[2][BK];
+  constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
+  __shared__ __attribute__((aligned(16))) T ks[NB][BK * LD];
+  __shared__ __attribute__((aligned(16))) T vs[NB][BK * LD];
+  __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
   const int split = blockIdx.x % splits;
   const int32_t rest = blockIdx.x / splits;
@@ -444,8 +439,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, i
   Piece kr[R::U], vr[R::U];
   float br[R::U];
   auto fetch = [&]() {
-    R::fetch(kr, a.k, rows, heads, tid, a.D, whole);
-    R::fetch(vr, a.v, rows, heads, tid, a.D, whole);
+    R::template fetch<WHOLE>(kr, a.k, rows, heads, tid, a.D);
+    R::template fetch<WHOLE>(vr, a.v, rows, heads, tid, a.D);
 #pragma unroll
     for (int u = 0; u < R::U; ++u) br[u] = rows[u] >= 0 ? 0.f : -INFINITY;
   };
@@ -467,15 +462,12 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, i
     }
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      qf[u][f].q = gf[u][f].q = u32x4{0u, 0u, 0u, 0u};
-      if (q[u].row >= 0) {
-        qf[u][f] = load_piece(row_of_head<const T>(a.q, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
-        gf[u][f] = load_piece(row_of_head<const T>(a.dout, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
-      }
+      qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
+      gf[u][f] = load_piece<T, WHOLE>(a.dout, q[u].row, q[u].h, f * KF + g4 * E, a.D);
     }
   }
   if constexpr (W > DP) {
-    for (int x = tid; x < 2 * BK; x += NT)
+    for (int x = tid; x < NB * BK; x += NT)
 #pragma unroll
       for (int e = DP; e < W; e += E) {
         *reinterpret_cast<u32x4*>(&ks[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
@@ -489,7 +481,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, i
 #pragma unroll
     for (int d = 0; d < DT; ++d) dq[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int32_t t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+    const int buf = NB == 1 ? 0 : (t - t0) & 1;
+    if constexpr (NB == 1) wave_sync();
     R::put(ks[buf], LD, kr, tid);
     R::put(vs[buf], LD, vr, tid);
     if (tid % R::PER == 0) {
@@ -497,7 +490,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, i
       for (int u = 0; u < R::U; ++u)
         if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[buf][R::row(tid, u)] = br[u];
     }
-    __syncthreads();
+    if constexpr (NB == 1) wave_sync();
+    else __syncthreads();
     if (t + 1 < t1) {
       fetch();
       number(t + 2);
@@ -551,7 +545,7 @@ __global__ __launch_bounds__(64 * NW) void k_attention_dq(Attn a, TileGrid tg, i
     }
     T* to = row_of_head<T>(a.dq, q[u].row, q[u].h);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) store4(to, d * 16 + g4 * 4, dq[u][d] * a.scale, a.D, whole_out);
+    for (int d = 0; d < DT; ++d) store4<T, WHOLE>(to, d * 16 + g4 * 4, dq[u][d] * a.scale, a.D);
   }
 }
 
@@ -625,34 +619,31 @@ Plan plan(const Attn& a, size_t size) {
   return p;
 }
 
-template <typename T, int DP, int KT> int group_launch(const Attn& a, bool whole, bool whole_out, hipStream_t st) {
-  k_attention_backward_group<T, DP, KT><<<dim3((uint32_t)ceil_div((int64_t)a.max_groups * a.K, 4)), 256, 0, st>>>(a, whole, whole_out);
+template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, hipStream_t st) {
+  k_attention_backward_group<T, DP, KT, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.max_groups * a.K, 4)), 256, 0, st>>>(a);
   return launch_status();
 }
-template <typename T, int DP> int run(Attn a, const Plan& p, char* ws, hipStream_t st) {
-  bool whole = true, whole_out = true;
-  for (const Heads* x : {&a.q, &a.k, &a.v, &a.out, &a.dout}) whole = whole && whole_pieces(*x, a.D, sizeof(T));
-  for (const Heads* x : {&a.dq, &a.dk, &a.dv}) whole_out = whole_out && whole_pieces(*x, a.D, sizeof(T));
+template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* ws, hipStream_t st) {
   if constexpr (DP <= 32) {
     if (p.group) {
       const int kt = (a.kl.G + 15) / 16;
-      if (kt <= 2) return group_launch<T, DP, 2>(a, whole, whole_out, st);
-      if (kt <= 4) return group_launch<T, DP, 4>(a, whole, whole_out, st);
-      if (kt <= 5) return group_launch<T, DP, 5>(a, whole, whole_out, st);
-      if (kt <= 6) return group_launch<T, DP, 6>(a, whole, whole_out, st);
-      return group_launch<T, DP, 8>(a, whole, whole_out, st);
+      if (kt <= 2) return group_launch<T, DP, 2, WHOLE>(a, st);
+      if (kt <= 4) return group_launch<T, DP, 4, WHOLE>(a, st);
+      if (kt <= 5) return group_launch<T, DP, 5, WHOLE>(a, st);
+      if (kt <= 6) return group_launch<T, DP, 6, WHOLE>(a, st);
+      return group_launch<T, DP, 8, WHOLE>(a, st);
     }
   }
   a.delta = reinterpret_cast<float*>(ws);
   float *pq = reinterpret_cast<float*>(ws + p.delta), *pk = reinterpret_cast<float*>(ws + p.delta + p.parts_q);
   if (a.ql.n > 0) {
     constexpr int PER = DP * (int)sizeof(T) / 16;
-    k_attention_delta<T, DP><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a, whole);
+    k_attention_delta<T, DP, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a);
     const dim3 grid((uint32_t)((int64_t)p.tq.tiles * a.K * p.splits_q));
     if (p.wide_q)
-      k_attention_dq<T, DP, 4, 2, 32><<<grid, 256, 0, st>>>(a, p.tq, p.splits_q, pq, whole, whole_out);
+      k_attention_dq<T, DP, 4, 2, 32, WHOLE><<<grid, 256, 0, st>>>(a, p.tq, p.splits_q, pq);
     else
-      k_attention_dq<T, DP, 1, 1, 32><<<grid, 64, 0, st>>>(a, p.tq, p.splits_q, pq, whole, whole_out);
+      k_attention_dq<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tq, p.splits_q, pq);
     if (p.splits_q > 1)
       k_attention_sum<T, DP, 1><<<dim3((uint32_t)ceil_div((int64_t)p.sum_q.tiles * a.H, 4)), 256, 0, st>>>(a, a.ql, p.sum_q, a.H, p.splits_q, pq, a.dq,
                                                                                                        a.dq, a.scale, a.scale);
@@ -660,21 +651,26 @@ template <typename T, int DP> int run(Attn a, const Plan& p, char* ws, hipStream
   if (a.kl.n > 0) {
     const dim3 grid((uint32_t)((int64_t)p.tk.tiles * a.K * p.splits_k));
     if (p.wide_k)
-      k_attention_dkv<T, DP, 4, 2><<<grid, 256, 0, st>>>(a, p.tk, p.splits_k, pk, whole, whole_out);
+      k_attention_dkv<T, DP, 4, 2, WHOLE><<<grid, 256, 0, st>>>(a, p.tk, p.splits_k, pk);
     else
-      k_attention_dkv<T, DP, 1, 1><<<grid, 64, 0, st>>>(a, p.tk, p.splits_k, pk, whole, whole_out);
+      k_attention_dkv<T, DP, 1, 1, WHOLE><<<grid, 64, 0, st>>>(a, p.tk, p.splits_k, pk);
     if (p.splits_k > 1)
       k_attention_sum<T, DP, 2><<<dim3((uint32_t)ceil_div((int64_t)p.sum_k.tiles * a.K, 4)), 256, 0, st>>>(a, a.kl, p.sum_k, a.K, p.splits_k, pk, a.dk,
                                                                                                        a.dv, a.scale, kLower<T>);
   }
   return launch_status();
 }
+template <typename T, int DP> int run_whole(const Attn& a, const Plan& p, char* ws, hipStream_t st) {
+  bool whole = true;
+  for (const Heads* x : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) whole = whole && whole_pieces(*x, a.D, sizeof(T));
+  return whole ? run<T, DP, true>(a, p, ws, st) : run<T, DP, false>(a, p, ws, st);
+}
 template <typename T> int run_type(const Attn& a, const Plan& p, char* ws, hipStream_t st) {
   switch (padded(a.D)) {
-    case 16: return run<T, 16>(a, p, ws, st);
-    case 32: return run<T, 32>(a, p, ws, st);
-    case 64: return run<T, 64>(a, p, ws, st);
-    default: return run<T, 128>(a, p, ws, st);
+    case 16: return run_whole<T, 16>(a, p, ws, st);
+    case 32: return run_whole<T, 32>(a, p, ws, st);
+    case 64: return run_whole<T, 64>(a, p, ws, st);
+    default: return run_whole<T, 128>(a, p, ws, st);
   }
 }
 

@@ -8,8 +8,8 @@ namespace {
 
 // ---- short groups: a wavefront holds all keys and values of a group and head ----------------------------------
 // Keys and values are read once into registers (values through LDS, which turns them), the queries go by 16 at a time.
-template <typename T, int DP, int KT>
-__global__ __launch_bounds__(256) void k_attention_group(Attn a, int parts, bool whole, bool whole_out) {
+template <typename T, int DP, int KT, bool WHOLE>
+__global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, int parts) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16;
   constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, LD = DP + 16 / (int)sizeof(T), PER = DP * (int)sizeof(T) / 16;
   __shared__ __attribute__((aligned(16))) T vs_all[4][RK * LD];
@@ -45,24 +45,17 @@ __global__ __launch_bounds__(256) void k_attention_group(Attn a, int parts, bool
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      kf[t][f].q = u32x4{0u, 0u, 0u, 0u};
-      if (key[t] >= 0) kf[t][f] = load_piece(row_of_head<const T>(a.k, key[t], kh), f * KF + g4 * E, a.D, whole);
-    }
+    for (int f = 0; f < NF; ++f) kf[t][f] = load_piece<T, WHOLE>(a.k, key[t], kh, f * KF + g4 * E, a.D);
   auto fetch_q = [&]() {
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      qf[f].q = u32x4{0u, 0u, 0u, 0u};
-      if (q.row >= 0) qf[f] = load_piece(row_of_head<const T>(a.q, q.row, q.h), f * KF + g4 * E, a.D, whole);
-    }
+    for (int f = 0; f < NF; ++f) qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
   };
   fetch_q();
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t)
 #pragma unroll
     for (int c = 0; c < (PER + 3) / 4; ++c) {
-      vr[t][c].q = u32x4{0u, 0u, 0u, 0u};
-      if (key[t] >= 0 && c * 4 + g4 < PER) vr[t][c] = load_piece(row_of_head<const T>(a.v, key[t], kh), (c * 4 + g4) * E, a.D, whole);
+      vr[t][c] = load_piece<T, WHOLE>(a.v, key[t], kh, (c * 4 + g4) * E, a.D);
     }
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t) {
@@ -125,7 +118,7 @@ __global__ __launch_bounds__(256) void k_attention_group(Attn a, int parts, bool
     const float by = sum == 0.f ? 0.f : 1.f / sum;  // no key: zero
     T* out = row_of_head<T>(a.out, now.row, now.h);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) store4(out, d * 16 + g4 * 4, o[d] * by, a.D, whole_out);
+    for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
     if (a.lse && g4 == 0) a.lse[(int64_t)now.row * a.H + now.h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
@@ -134,14 +127,21 @@ __global__ __launch_bounds__(256) void k_attention_group(Attn a, int parts, bool
 // NW wavefronts of QT x 16 rows of queries each.  Tiles of BK keys lie twice in LDS: one is read while the next one is written, its
 // rows fetched into registers a tile ahead and their numbers two.  splits > 1: each workgroup takes a stretch of a group's keys and
 // leaves sums, maximum and total in the workspace; k_attention_join brings them together.
-template <typename T, int DP, int NW, int QT, int BK>
-__global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg, int splits, float* part, bool whole, bool whole_out) {
+//
+// The vector unit is what such a kernel waits for (an exponential takes as long as four other instructions), so little else is done a
+// score.  The products of a tile start from minus the running maximum instead of zero.  That maximum may be too low by a factor of
+// 2^8 in p (no type's range minds), so that lanes need not compare notes: only where a lane finds a score beyond that, or its row has
+// met no key yet, is the maximum made good and what was summed brought down.   Keys that are not there cost something in their own tiles
+// only.  The sum of p is one of float32 additions: a product with ones would sum the rounded p, and lse would be 2^-9 off.
+template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) || (DP == 64 && NW == 4) ? 2 : 1) void k_attention_tiles(Attn a, TileGrid tg, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int KW = NF * KF, LDK = KW + 16 / (int)sizeof(T), LDV = DP + 32 / (int)sizeof(T), BQ = 16 * QT * NW;
+  constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
   typedef Rows<T, DP, BK, NT> R;
-  __shared__ __attribute__((aligned(16))) T ks[2][BK * LDK];
-  __shared__ __attribute__((aligned(16))) T vs[2][BK * LDV];
-  __shared__ __attribute__((aligned(16))) float bias[2][BK];
+  __shared__ __attribute__((aligned(16))) T ks[NB][BK * LDK];
+  __shared__ __attribute__((aligned(16))) T vs[NB][BK * LDV];
+  __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
   const int split = blockIdx.x % splits;
   const int32_t rest = blockIdx.x / splits;
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
   Piece kr[R::U], vr[R::U];
   float br[R::U];
   auto fetch = [&]() {
-    R::fetch(kr, a.k, rows, heads, tid, a.D, whole);
-    R::fetch(vr, a.v, rows, heads, tid, a.D, whole);
+    R::template fetch<WHOLE>(kr, a.k, rows, heads, tid, a.D);
+    R::template fetch<WHOLE>(vr, a.v, rows, heads, tid, a.D);
 #pragma unroll
     for (int u = 0; u < R::U; ++u) br[u] = rows[u] >= 0 ? 0.f : -INFINITY;
   };
@@ -183,26 +183,30 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
   for (int u = 0; u < QT; ++u)
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      qf[u][f].q = u32x4{0u, 0u, 0u, 0u};
-      if (q[u].row >= 0) qf[u][f] = load_piece(row_of_head<const T>(a.q, q[u].row, q[u].h), f * KF + g4 * E, a.D, whole);
+      qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
+      if (a.scale < 0.f) qf[u][f] = negated<T>(qf[u][f]);
     }
   if constexpr (KW > DP) {  // columns behind the rows' ends: zero in both operands
-    for (int x = tid; x < 2 * BK; x += NT)
+    for (int x = tid; x < NB * BK; x += NT)
 #pragma unroll
       for (int e = DP; e < KW; e += E) *reinterpret_cast<u32x4*>(&ks[0][0] + x * LDK + e) = u32x4{0u, 0u, 0u, 0u};
   }
-  const float c = a.scale * kLog2e;
-  f32x4 o[QT][DT];
-  float top[QT], sum[QT];
+  // scores as they come from the products grow with the exponents: c > 0 (a scale of zero as next to nothing)
+  const float c = a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e, far = 8.f / c;
+  f32x4 o[QT][DT], sum[QT];
+  float base[QT];  // minus the running maximum of the scores
+  bool met[QT];    // whether the row has met a key
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
-    top[u] = kLowest;
-    sum[u] = 0.f;
+    base[u] = 0.f;
+    met[u] = false;
+    sum[u] = all4(0.f);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[u][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; ++d) o[u][d] = all4(0.f);
   }
   for (int32_t t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
+    const int buf = NB == 1 ? 0 : (t - t0) & 1;
+    if constexpr (NB == 1) wave_sync();
     R::put(ks[buf], LDK, kr, tid);
     R::put(vs[buf], LDV, vr, tid);
     if (tid % R::PER == 0) {
@@ -210,16 +214,18 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
       for (int u = 0; u < R::U; ++u)
         if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[buf][R::row(tid, u)] = br[u];
     }
-    __syncthreads();
+    if constexpr (NB == 1) wave_sync();
+    else __syncthreads();
     if (t + 1 < t1) {
       fetch();
       number(t + 2);
     }
+    const bool gaps = __any(bias[buf][lane % BK] < 0.f);
     f32x4 s[QT][BK / 16];
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k) {
 #pragma unroll
-      for (int u = 0; u < QT; ++u) s[u][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < QT; ++u) s[u][k] = all4(base[u]);
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         const Piece kf = row_piece(ks[buf], LDK, k * 16 + i, f * KF + g4 * E);
@@ -227,33 +233,51 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
         for (int u = 0; u < QT; ++u) s[u][k] = mma<T>(kf, qf[u][f], s[u][k]);
       }
     }
-    Piece p[QT][BK / 16 / TILES];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      float m = top[u];
+    if (gaps) {
 #pragma unroll
       for (int k = 0; k < BK / 16; ++k) {
         const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + k * 16 + g4 * 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[u][k][r] = fmaf(s[u][k][r], c, b[r]);
-          m = fmaxf(m, s[u][k][r]);
-        }
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[u][k][r] = b[r] < 0.f ? -INFINITY : s[u][k][r];
       }
-      m = over_lanes16_max(m);
-      if (__any(m > top[u])) {  // after the first tiles the maximum seldom grows
-        const float f = exp2_fast(top[u] - m);
+    }
+    bool raise = false;
+    float top[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      top[u] = s[u][0][0];
+#pragma unroll
+      for (int k = 0; k < BK / 16; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top[u] = fmaxf(top[u], s[u][k][r]);
+      raise |= top[u] > far || !met[u];
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+        const float m = over_lanes16_max(top[u]);  // above the maximum so far
+        const bool up = m > (met[u] ? 0.f : -INFINITY);
+        const float by = up ? m : 0.f, f = met[u] ? exp2_fast(-c * by) : 0.f;
         sum[u] *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[u][d] *= f;
-        top[u] = m;
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k) s[u][k] -= by;
+        base[u] -= by;
+        met[u] |= up;
       }
+    }
+    Piece p[QT][BK / 16 / TILES];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
 #pragma unroll
       for (int k = 0; k < BK / 16; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[u][k][r] = exp2_fast(s[u][k][r] - m);
-          sum[u] += s[u][k][r];
+          s[u][k][r] = exp2_fast(s[u][k][r] * c);
+          sum[u][r] += s[u][k][r];
         }
 #pragma unroll
       for (int k = 0; k < BK / 16 / TILES; ++k) p[u][k] = as_piece<T>(s[u] + k * TILES);
@@ -269,7 +293,8 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
-    const float total = over_lanes16_sum(sum[u]);
+    const float total = over_lanes16_sum((sum[u][0] + sum[u][1]) + (sum[u][2] + sum[u][3]));
+    const float top = met[u] ? -c * base[u] : kLowest;
     if (q[u].row < 0) continue;
     const int64_t at_row = (int64_t)q[u].row * a.H + q[u].h;
     if (splits > 1) {
@@ -279,7 +304,7 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(po + d * 16 + g4 * 4) = o[u][d];
       if (g4 == 0) {
-        ml[0] = top[u];
+        ml[0] = top;
         ml[1] = total;
       }
       continue;
@@ -287,15 +312,20 @@ __global__ __launch_bounds__(64 * NW) void k_attention_tiles(Attn a, TileGrid tg
     const float by = total == 0.f ? 0.f : 1.f / total;  // no key: zero
     T* out = row_of_head<T>(a.out, q[u].row, q[u].h);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) store4(out, d * 16 + g4 * 4, o[u][d] * by, a.D, whole_out);
-    if (a.lse && g4 == 0) a.lse[at_row] = total == 0.f ? -INFINITY : (top[u] + __builtin_amdgcn_logf(total)) * kLn2;
+    for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[u][d] * by, a.D);
+    if (a.lse && g4 == 0) a.lse[at_row] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
   }
 }
 
-// One workgroup of four wavefronts a row and head: each joins every fourth stretch, then the four.
+constexpr int kMostSplits = 512;  // of a group's keys
+
+// The stretches of one row and head.  A few lanes hold a stretch's sums, four elements each, so that a workgroup's loads cover many
+// stretches at once; their weights are worked out first, a stretch a thread.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int splits, const float* part) {
-  __shared__ float tops[4], sums[4], os[4][DP];
+  constexpr int LANES = DP / 4, AT_ONCE = 256 / LANES;
+  __shared__ float weight[kMostSplits], tops[4], sums[4];
+  __shared__ __attribute__((aligned(16))) float os[AT_ONCE][DP];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kh = blockIdx.x / tg.tiles;
   const TileAt at = tile_at<1>(a, a.ql, tg, blockIdx.x - kh * tg.tiles, lane);
@@ -303,38 +333,45 @@ __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int
   const QueryRow q = query_row(a, span_of(a.ql, at.g), tg.share, kh, at.tile);
   if (q.row < 0) return;
   const int64_t all = (int64_t)a.ql.n * a.H, at_row = (int64_t)q.row * a.H + q.h;
-  const float *ml = part + at_row * 2, *po = part + splits * all * 2 + at_row * DP;
-  float top = kLowest, sum = 0.f, o[(DP + 63) / 64] = {};
-  for (int s = wave; s < splits; s += 4) top = fmaxf(top, ml[s * all * 2]);
-  for (int s = wave; s < splits; s += 4) {
-    const float f = exp2_fast(ml[s * all * 2] - top);
-    sum += f * ml[s * all * 2 + 1];
+  const float2* const ml = reinterpret_cast<const float2*>(part) + at_row;
+  const float* const po = part + splits * all * 2 + at_row * DP + tid % LANES * 4;
+  constexpr int MINE = kMostSplits / 256;
+  float2 mine[MINE];
+  float top = kLowest;
 #pragma unroll
-    for (int e = 0; e < (DP + 63) / 64; ++e)
-      if (e * 64 + lane < DP) o[e] = fmaf(f, po[s * all * DP + e * 64 + lane], o[e]);
-  }
-  if (lane == 0) {
-    tops[wave] = top;
-    sums[wave] = sum;
+  for (int s = 0; s < MINE; ++s) {
+    mine[s] = s * 256 + tid < splits ? ml[(s * 256 + tid) * all] : make_float2(kLowest, 0.f);
+    top = fmaxf(top, mine[s].x);
   }
 #pragma unroll
-  for (int e = 0; e < (DP + 63) / 64; ++e)
-    if (e * 64 + lane < DP) os[wave][e * 64 + lane] = o[e];
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) tops[wave] = top;
   __syncthreads();
-  const float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  float f[4], total = 0.f;
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float total = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    f[w] = exp2_fast(tops[w] - m);
-    total += f[w] * sums[w];
+  for (int s = 0; s < MINE; ++s) {
+    const float f = exp2_fast(mine[s].x - top);
+    if (s * 256 + tid < splits) weight[s * 256 + tid] = f;
+    total = fmaf(f, mine[s].y, total);
   }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = tid / LANES; s < splits; s += AT_ONCE) o += *reinterpret_cast<const f32x4*>(po + s * all * DP) * weight[s];
+  *reinterpret_cast<f32x4*>(&os[tid / LANES][tid % LANES * 4]) = o;
+  __syncthreads();
   if (tid < a.D) {
     float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) v = fmaf(f[w], os[w][tid], v);
+#pragma unroll 8
+    for (int s = 0; s < AT_ONCE; ++s) v += os[s][tid];
     Elem<T>::store(row_of_head<T>(a.out, q.row, q.h) + tid, total == 0.f ? 0.f : v / total);
   }
-  if (tid == 0 && a.lse) a.lse[at_row] = total == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(total)) * kLn2;
+  if (tid == 0 && a.lse) a.lse[at_row] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
 // ---- which kernel ---------------------------------------------------------------------------------------
@@ -367,6 +404,7 @@ Plan plan(const Attn& a, size_t size) {
   int64_t s = groups ? ceil_div(p.wide ? 2 * kChipWaves : kChipWaves, waves ? waves : 1) : 1;
   const int64_t most = a.kl.G / 256 > 0 ? a.kl.G / 256 : 1;
   if (s > most) s = most;
+  if (s > kMostSplits) s = kMostSplits;
   if (waves * 2 > kChipWaves) s = 1;
   p.splits = (int)s;
   p.fits = p.fits && groups * s <= INT32_MAX;
@@ -379,38 +417,41 @@ Plan plan(const Attn& a, size_t size) {
   return p;
 }
 
-template <typename T, int DP, int KT> int group_launch(const Attn& a, const Plan& p, bool whole, bool whole_out, hipStream_t st) {
+template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, const Plan& p, hipStream_t st) {
   const int64_t waves = (int64_t)a.max_groups * a.K * p.parts;
-  k_attention_group<T, DP, KT><<<dim3((uint32_t)ceil_div(waves, 4)), 256, 0, st>>>(a, p.parts, whole, whole_out);
+  k_attention_group<T, DP, KT, WHOLE><<<dim3((uint32_t)ceil_div(waves, 4)), 256, 0, st>>>(a, p.parts);
   return launch_status();
 }
-template <typename T, int DP> int run(const Attn& a, const Plan& p, float* ws, hipStream_t st) {
-  const bool whole = whole_pieces(a.q, a.D, sizeof(T)) && whole_pieces(a.k, a.D, sizeof(T)) && whole_pieces(a.v, a.D, sizeof(T));
-  const bool whole_out = whole_pieces(a.out, a.D, sizeof(T));
+template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, float* ws, hipStream_t st) {
   if constexpr (DP <= (sizeof(T) == 4 ? 32 : 64)) {
     if (p.group) {
       const int kt = (a.kl.G + 15) / 16;
-      if (kt <= 2) return group_launch<T, DP, 2>(a, p, whole, whole_out, st);
-      if (kt <= 4) return group_launch<T, DP, 4>(a, p, whole, whole_out, st);
-      if (kt <= 5) return group_launch<T, DP, 5>(a, p, whole, whole_out, st);
-      if (kt <= 6) return group_launch<T, DP, 6>(a, p, whole, whole_out, st);
-      return group_launch<T, DP, 8>(a, p, whole, whole_out, st);
+      if (kt <= 2) return group_launch<T, DP, 2, WHOLE>(a, p, st);
+      if (kt <= 4) return group_launch<T, DP, 4, WHOLE>(a, p, st);
+      if (kt <= 5) return group_launch<T, DP, 5, WHOLE>(a, p, st);
+      if (kt <= 6) return group_launch<T, DP, 6, WHOLE>(a, p, st);
+      return group_launch<T, DP, 8, WHOLE>(a, p, st);
     }
   }
   const dim3 grid((uint32_t)((int64_t)p.tg.tiles * a.K * p.splits));
   if (p.wide)
-    k_attention_tiles<T, DP, 4, 2, 64><<<grid, 256, 0, st>>>(a, p.tg, p.splits, ws, whole, whole_out);
+    k_attention_tiles<T, DP, 4, 2, 64, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, p.splits, ws);
   else
-    k_attention_tiles<T, DP, 1, 1, 32><<<grid, 64, 0, st>>>(a, p.tg, p.splits, ws, whole, whole_out);
+    k_attention_tiles<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tg, p.splits, ws);
   if (p.splits > 1) k_attention_join<T, DP><<<dim3((uint32_t)((int64_t)p.join.tiles * a.K)), 256, 0, st>>>(a, p.join, p.splits, ws);
   return launch_status();
 }
+template <typename T, int DP> int run_whole(const Attn& a, const Plan& p, float* ws, hipStream_t st) {
+  bool whole = true;
+  for (const Heads* x : {&a.q, &a.k, &a.v, &a.out}) whole = whole && whole_pieces(*x, a.D, sizeof(T));
+  return whole ? run<T, DP, true>(a, p, ws, st) : run<T, DP, false>(a, p, ws, st);
+}
 template <typename T> int run_type(const Attn& a, const Plan& p, float* ws, hipStream_t st) {
   switch (padded(a.D)) {
-    case 16: return run<T, 16>(a, p, ws, st);
-    case 32: return run<T, 32>(a, p, ws, st);
-    case 64: return run<T, 64>(a, p, ws, st);
-    default: return run<T, 128>(a, p, ws, st);
+    case 16: return run_whole<T, 16>(a, p, ws, st);
+    case 32: return run_whole<T, 32>(a, p, ws, st);
+    case 64: return run_whole<T, 64>(a, p, ws, st);
+    default: return run_whole<T, 128>(a, p, ws, st);
   }
 }
 

@@ -75,8 +75,8 @@ template <> __device__ __forceinline__ Piece as_piece<float>(const f32x4* t) {
 }
 
 // Four elements side by side (one lane's part of a result tile) into memory, those from D on left out
-template <typename T> __device__ __forceinline__ void store4(T* row, int e, f32x4 v, int D, bool whole) {
-  if (whole) {
+template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T* row, int e, f32x4 v, int D) {
+  if constexpr (WHOLE) {
     if (e >= D) return;
     if constexpr (sizeof(T) == 4) {
       *reinterpret_cast<f32x4*>(row + e) = v;
@@ -92,22 +92,27 @@ template <typename T> __device__ __forceinline__ void store4(T* row, int e, f32x
   }
 }
 
-// 16 bytes of a row from element e on, zero from D on.  whole: rows are 16-byte pieces, from their addresses to their ends.
-template <typename T> __device__ __forceinline__ Piece load_piece(const T* row, int e, int D, bool whole) {
+__device__ const u32x4 kZeroPiece = {0u, 0u, 0u, 0u};
+
+// 16 bytes of row `row` (negative: none) and head h from element e on, zero from D on.  WHOLE: rows are pieces of 16 bytes, from their
+// addresses to their ends; what is not there is then read from a piece of zeros, so that a wavefront asks for all its pieces at once.
+template <typename T, bool WHOLE> __device__ __forceinline__ Piece load_piece(const Heads& x, int32_t row, int32_t h, int e, int D) {
   Piece p;
-  p.q = u32x4{0u, 0u, 0u, 0u};
-  if (whole) {
-    if (e < D) p.q = *reinterpret_cast<const u32x4*>(row + e);
+  const T* at = row_of_head<const T>(x, row, h) + e;
+  if constexpr (WHOLE) {
+    p.q = *(row >= 0 && e < D ? reinterpret_cast<const u32x4*>(at) : &kZeroPiece);
   } else {
+    p.q = u32x4{0u, 0u, 0u, 0u};
+    if (row < 0) return p;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (e + j < D) p.f[j] = row[e + j];
+        if (e + j < D) p.f[j] = at[j];
     } else {
-      const uint16_t* x = reinterpret_cast<const uint16_t*>(row);
+      const uint16_t* x16 = reinterpret_cast<const uint16_t*>(at);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (e + j < D) p.q[j / 2] |= (uint32_t)x[e + j] << (16 * (j % 2));
+        if (e + j < D) p.q[j / 2] |= (uint32_t)x16[j] << (16 * (j % 2));
     }
   }
   return p;
@@ -140,6 +145,13 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+
+template <typename T> __device__ __forceinline__ Piece negated(Piece p) {
+  const uint32_t sign = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+  p.q ^= u32x4{sign, sign, sign, sign};
+  return p;
+}
+__device__ __forceinline__ f32x4 all4(float v) { return f32x4{v, v, v, v}; }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float over_lanes16_max(float v) {  // over the four lanes of a column
@@ -194,13 +206,10 @@ template <typename T, int DP, int R, int NT> struct Rows {
   static constexpr int U = (R * PER + NT - 1) / NT;                 // pieces of a thread
   static constexpr int STEP = NT / PER;                             // rows between two pieces of a thread
   static __device__ __forceinline__ int row(int tid, int u) { return tid / PER + u * STEP; }
-  static __device__ __forceinline__ void fetch(Piece (&r)[U], const Heads& x, const int32_t (&rows)[U], const int32_t (&heads)[U], int tid,
-                                               int D, bool whole) {
+  template <bool WHOLE>
+  static __device__ __forceinline__ void fetch(Piece (&r)[U], const Heads& x, const int32_t (&rows)[U], const int32_t (&heads)[U], int tid, int D) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      r[u].q = u32x4{0u, 0u, 0u, 0u};
-      if (rows[u] >= 0) r[u] = load_piece(row_of_head<const T>(x, rows[u], heads[u]), (tid % PER) * Mx<T>::E, D, whole);
-    }
+    for (int u = 0; u < U; ++u) r[u] = load_piece<T, WHOLE>(x, rows[u], heads[u], (tid % PER) * Mx<T>::E, D);
   }
   static __device__ __forceinline__ void put(T* tile, int ld, const Piece (&r)[U], int tid) {
 #pragma unroll
