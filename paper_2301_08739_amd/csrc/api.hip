@@ -97,7 +97,8 @@ bool meets_written(const HeadsIn* arrays, int count, size_t size, const void* p,
     if (arrays[i].written && arrays[i].n > 0 && overlaps(arrays[i].x->data, (size_t)span_elems(arrays[i]) * size, p, bytes)) return true;
   return false;
 }
-Heads heads_of(const ff_heads* x) { return {x->data, x->row_stride, x->head_stride}; }
+HeadsAt heads_at(const ff_heads* x) { return {x->data, x->row_stride, x->head_stride}; }
+Heads heads_of(const ff_heads* x, size_t size) { return {(char*)x->data, x->head_stride * (int64_t)size, (uint32_t)(x->row_stride * size)}; }
 
 int check_list(const ff_group_list& l) {
   if (l.n < 0 || l.G < 1) return FF_ERR_ARG;
@@ -122,6 +123,8 @@ int check_attention_call(const ff_attention_shape* a, const HeadsIn* arrays, int
                          const void* workspace, size_t workspace_bytes, size_t need) {
   const size_t size = elem_size(dtype), lse_bytes = (size_t)a->queries.n * a->heads * 4;
   if (const int st = check_arrays(arrays, count, size); st != FF_OK) return st;
+  for (int i = 0; i < count; ++i)
+    if (arrays[i].x->row_stride > (int64_t)(UINT32_MAX / size)) return FF_ERR_UNSUPPORTED;
   if ((a->max_groups > 0 && (!a->queries.offsets || !a->keys.offsets)) || (uintptr_t)lse % 4) return FF_ERR_ARG;
   const struct { const void* p; size_t bytes; bool written; } pieces[] = {
       {lse, lse_bytes, lse_written}, {workspace, need, true},
@@ -584,7 +587,7 @@ int ff_attention(const ff_attention_shape* a, const ff_heads* q, const ff_heads*
   const size_t need = attention_workspace_bytes(t, dtype);
   if (const int st = check_attention_call(a, arrays, 4, dtype, lse, true, workspace, workspace_bytes, need); st != FF_OK) return st;
   if (t.ql.n == 0 || t.max_groups == 0) return FF_OK;
-  t.q = heads_of(q); t.k = heads_of(k); t.v = heads_of(v); t.out = heads_of(out);
+  t.q = heads_of(q, elem_size(dtype)); t.k = heads_of(k, elem_size(dtype)); t.v = heads_of(v, elem_size(dtype)); t.out = heads_of(out, elem_size(dtype));
   t.lse = lse;
   return attention_launch(t, dtype, workspace, (hipStream_t)stream);
 }
@@ -607,8 +610,8 @@ int ff_attention_backward(const ff_attention_shape* a, const ff_heads* q, const 
   const size_t need = attention_backward_workspace_bytes(t, dtype);
   if (const int st = check_attention_call(a, arrays, 8, dtype, lse, false, workspace, workspace_bytes, need); st != FF_OK) return st;
   if (t.max_groups == 0 || (t.ql.n == 0 && t.kl.n == 0)) return FF_OK;
-  t.q = heads_of(q); t.k = heads_of(k); t.v = heads_of(v); t.out = heads_of(out); t.dout = heads_of(dout);
-  t.dq = heads_of(dq); t.dk = heads_of(dk); t.dv = heads_of(dv);
+  t.q = heads_of(q, elem_size(dtype)); t.k = heads_of(k, elem_size(dtype)); t.v = heads_of(v, elem_size(dtype)); t.out = heads_of(out, elem_size(dtype)); t.dout = heads_of(dout, elem_size(dtype));
+  t.dq = heads_of(dq, elem_size(dtype)); t.dk = heads_of(dk, elem_size(dtype)); t.dv = heads_of(dv, elem_size(dtype));
   t.lse = const_cast<float*>(lse);
   return attention_backward_launch(t, dtype, workspace, (hipStream_t)stream);
 }
@@ -641,8 +644,8 @@ int ff_rotary(const ff_heads* q, const ff_heads* q_out, int32_t q_heads, const f
     return FF_ERR_ARG;
   if (n == 0) return FF_OK;
   Rotary r{};
-  r.q = heads_of(q); r.q_out = heads_of(q_out);
-  if (k) { r.k = heads_of(k); r.k_out = heads_of(k_out); }
+  r.q = heads_at(q); r.q_out = heads_at(q_out);
+  if (k) { r.k = heads_at(k); r.k_out = heads_at(k_out); }
   r.q_heads = q_heads; r.k_heads = k_heads; r.D = head_dim; r.n = n;
   r.pos = positions; r.pos_rs = position_row_stride; r.pos_as = position_axis_stride;
   r.freqs = spec->freqs; r.axes = spec->axes; r.pairs = spec->pairs; r.layout = spec->layout;

@@ -4,9 +4,10 @@
 
 namespace ff {
 
-struct Heads {  // element e of head h of row r: p[r * rs + h * hs + e]
-  void* p;
-  int64_t rs, hs;
+struct Heads {  // head h of row r begins r * rs + h * hs bytes on
+  char* p;
+  int64_t hs;
+  uint32_t rs;  // (so that an address is one multiplication and addition: rows of 4 GiB and more are refused)
 };
 struct GroupList {
   const int32_t* perm;  // or nullptr: position p is row p
@@ -30,8 +31,12 @@ int attention_launch(const Attn& a, int dtype, void* workspace, hipStream_t stre
 size_t attention_backward_workspace_bytes(const Attn& a, int dtype);
 int attention_backward_launch(const Attn& a, int dtype, void* workspace, hipStream_t stream);
 
+struct HeadsAt {  // element e of head h of row r: p[r * rs + h * hs + e]
+  void* p;
+  int64_t rs, hs;
+};
 struct Rotary {
-  Heads q, q_out, k, k_out;
+  HeadsAt q, q_out, k, k_out;
   int32_t q_heads, k_heads, D;
   int64_t n;
   const int32_t* pos;
@@ -60,7 +65,7 @@ __device__ __forceinline__ int32_t row_at(const GroupList& l, int32_t p) {
   return (uint32_t)r < (uint32_t)l.n ? r : -1;
 }
 template <typename T> __device__ __forceinline__ T* row_of_head(const Heads& x, int32_t row, int32_t h) {
-  return reinterpret_cast<T*>(x.p) + (int64_t)row * x.rs + (int64_t)h * x.hs;
+  return reinterpret_cast<T*>(x.p + h * x.hs + (uint64_t)(uint32_t)row * x.rs);
 }
 
 }  // namespace ff

@@ -264,24 +264,30 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
       const int r = R::row(tid, u);
-      QueryRow q = {-1, 0};
-      if (t < t1 && r < BQ) q = query_row(a, sq, share, kh, t * BQ + r);
-      rows[u] = q.row;
-      heads[u] = q.h;
+      const int32_t v = t * BQ + r, p = share == 1 ? v : v / share;
+      rows[u] = t < t1 && r < BQ && p < sq.len ? sq.at + p : -1;
+      heads[u] = kh * share + (share == 1 ? 0 : v - p * share);
+    }
+    if (a.ql.perm) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u) rows[u] = rows[u] < 0 ? -1 : a.ql.perm[rows[u]];
     }
   };
   Piece qr[R::U], gr[R::U];
   float fo[R::U], fd[R::U];
-  auto fetch = [&]() {
+  auto fetch = [&]() {  // (numbers are looked at here, not where they are asked for: nothing waits for what it has just asked for)
+#pragma unroll
+    for (int u = 0; u < R::U; ++u)
+      if ((uint32_t)rows[u] >= (uint32_t)a.ql.n) rows[u] = -1;
     R::template fetch<WHOLE>(qr, a.q, rows, heads, tid, a.D);
     R::template fetch<WHOLE>(gr, a.dout, rows, heads, tid, a.D);
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
-      fo[u] = INFINITY;
+      fo[u] = -INFINITY;
       fd[u] = 0.f;
       if (tid % R::PER == 0 && rows[u] >= 0) {
-        fo[u] = as_offset<T>(a.lse[(int64_t)rows[u] * a.H + heads[u]]);
-        fd[u] = a.delta[(int64_t)rows[u] * a.H + heads[u]] * kLower<T>;
+        fo[u] = a.lse[(int64_t)rows[u] * a.H + heads[u]];
+        fd[u] = a.delta[(int64_t)rows[u] * a.H + heads[u]];
       }
     }
   };
@@ -327,8 +333,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
 #pragma unroll
       for (int u = 0; u < R::U; ++u)
         if (BQ * R::PER % NT == 0 || R::row(tid, u) < BQ) {
-          offs[buf][R::row(tid, u)] = fo[u];
-          deltas[buf][R::row(tid, u)] = fd[u];
+          offs[buf][R::row(tid, u)] = as_offset<T>(fo[u]);
+          deltas[buf][R::row(tid, u)] = fd[u] * kLower<T>;
         }
     }
     if constexpr (NB == 1) wave_sync();
@@ -409,7 +415,6 @@ template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(Attn a, TileGrid tg, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T), BQ = 16 * QT * NW;
-  typedef Rows<T, DP, BK, NT> R;
   constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
   __shared__ __attribute__((aligned(16))) T ks[NB][BK * LD];
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LD];
@@ -425,31 +430,13 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   const int32_t tiles = (sk.len + BK - 1) / BK, per = (tiles + splits - 1) / splits;
   const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-  int32_t rows[R::U], heads[R::U];
-  auto number = [&](int32_t t) {
-#pragma unroll
-    for (int u = 0; u < R::U; ++u) {
-      const int r = R::row(tid, u);
-      const int32_t p = t * BK + r;
-      rows[u] = t < t1 && r < BK && p < sk.len ? row_at(a.kl, sk.at + p) : -1;
-      heads[u] = kh;
-      if (a.mask && rows[u] >= 0 && !a.mask[rows[u]]) rows[u] = -1;
-    }
-  };
-  Piece kr[R::U], vr[R::U];
-  float br[R::U];
-  auto fetch = [&]() {
-    R::template fetch<WHOLE>(kr, a.k, rows, heads, tid, a.D);
-    R::template fetch<WHOLE>(vr, a.v, rows, heads, tid, a.D);
-#pragma unroll
-    for (int u = 0; u < R::U; ++u) br[u] = rows[u] >= 0 ? 0.f : -INFINITY;
-  };
-  number(t0);
+  KeyTiles<T, DP, BK, NT> kt;
+  kt.next(a, sk, t0, t1, tid);
   QueryRow q[QT];
 #pragma unroll
   for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
-  fetch();
-  number(t0 + 1);
+  kt.template fetch<WHOLE>(a, kh, tid);
+  kt.next(a, sk, t0 + 1, t1, tid);
   Piece qf[QT][NF], gf[QT][NF];
   float off[QT], delta[QT];
 #pragma unroll
@@ -483,18 +470,12 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   for (int32_t t = t0; t < t1; ++t) {
     const int buf = NB == 1 ? 0 : (t - t0) & 1;
     if constexpr (NB == 1) wave_sync();
-    R::put(ks[buf], LD, kr, tid);
-    R::put(vs[buf], LD, vr, tid);
-    if (tid % R::PER == 0) {
-#pragma unroll
-      for (int u = 0; u < R::U; ++u)
-        if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[buf][R::row(tid, u)] = br[u];
-    }
+    kt.put(a, ks[buf], LD, vs[buf], LD, bias[buf], tid);
     if constexpr (NB == 1) wave_sync();
     else __syncthreads();
     if (t + 1 < t1) {
-      fetch();
-      number(t + 2);
+      kt.template fetch<WHOLE>(a, kh, tid);
+      kt.next(a, sk, t + 2, t1, tid);
     }
 #pragma unroll
     for (int k = 0; k < BK / 16 / TILES; ++k) {

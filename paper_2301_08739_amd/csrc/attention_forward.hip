@@ -2,6 +2,7 @@
 // probabilities in registers only.  Scores are computed with the keys down and the queries across (K Q^T), so that a lane holds
 // scores of one query, and the probabilities are the right operand of (out)^T = V^T P^T as they lie in the registers.
 #include "attention_mx.h"
+#include <type_traits>
 
 namespace ff {
 namespace {
@@ -138,7 +139,6 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int KW = NF * KF, LDK = KW + 16 / (int)sizeof(T), LDV = DP + 32 / (int)sizeof(T), BQ = 16 * QT * NW;
   constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
-  typedef Rows<T, DP, BK, NT> R;
   __shared__ __attribute__((aligned(16))) T ks[NB][BK * LDK];
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LDV];
   __shared__ __attribute__((aligned(16))) float bias[NB][BK];
@@ -153,32 +153,14 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   const int32_t tiles = (sk.len + BK - 1) / BK, per = (tiles + splits - 1) / splits;
   const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
-  int32_t rows[R::U], heads[R::U];
-  auto number = [&](int32_t t) {
-#pragma unroll
-    for (int u = 0; u < R::U; ++u) {
-      const int r = R::row(tid, u);
-      const int32_t p = t * BK + r;
-      rows[u] = t < t1 && r < BK && p < sk.len ? row_at(a.kl, sk.at + p) : -1;
-      heads[u] = kh;
-      if (a.mask && rows[u] >= 0 && !a.mask[rows[u]]) rows[u] = -1;
-    }
-  };
-  Piece kr[R::U], vr[R::U];
-  float br[R::U];
-  auto fetch = [&]() {
-    R::template fetch<WHOLE>(kr, a.k, rows, heads, tid, a.D);
-    R::template fetch<WHOLE>(vr, a.v, rows, heads, tid, a.D);
-#pragma unroll
-    for (int u = 0; u < R::U; ++u) br[u] = rows[u] >= 0 ? 0.f : -INFINITY;
-  };
-  number(t0);
+  KeyTiles<T, DP, BK, NT> kt;
+  kt.next(a, sk, t0, t1, tid);
   QueryRow q[QT];
   Piece qf[QT][NF];
 #pragma unroll
   for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
-  fetch();
-  number(t0 + 1);
+  kt.template fetch<WHOLE>(a, kh, tid);
+  kt.next(a, sk, t0 + 1, t1, tid);
 #pragma unroll
   for (int u = 0; u < QT; ++u)
 #pragma unroll
@@ -194,33 +176,17 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   // scores as they come from the products grow with the exponents: c > 0 (a scale of zero as next to nothing)
   const float c = a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e, far = 8.f / c;
   f32x4 o[QT][DT], sum[QT];
-  float base[QT];  // minus the running maximum of the scores
-  bool met[QT];    // whether the row has met a key
+  float base[QT];   // minus the running maximum of the scores
+  float limit[QT];  // what a score above it may reach: -infinity until the row has met a key
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
     base[u] = 0.f;
-    met[u] = false;
+    limit[u] = -INFINITY;
     sum[u] = all4(0.f);
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[u][d] = all4(0.f);
   }
-  for (int32_t t = t0; t < t1; ++t) {
-    const int buf = NB == 1 ? 0 : (t - t0) & 1;
-    if constexpr (NB == 1) wave_sync();
-    R::put(ks[buf], LDK, kr, tid);
-    R::put(vs[buf], LDV, vr, tid);
-    if (tid % R::PER == 0) {
-#pragma unroll
-      for (int u = 0; u < R::U; ++u)
-        if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[buf][R::row(tid, u)] = br[u];
-    }
-    if constexpr (NB == 1) wave_sync();
-    else __syncthreads();
-    if (t + 1 < t1) {
-      fetch();
-      number(t + 2);
-    }
-    const bool gaps = __any(bias[buf][lane % BK] < 0.f);
+  auto tile = [&](auto with_gaps, const T* kb, const T* vb, const float* bb) {
     f32x4 s[QT][BK / 16];
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k) {
@@ -228,15 +194,12 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       for (int u = 0; u < QT; ++u) s[u][k] = all4(base[u]);
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
-        const Piece kf = row_piece(ks[buf], LDK, k * 16 + i, f * KF + g4 * E);
+        const Piece kf = row_piece(kb, LDK, k * 16 + i, f * KF + g4 * E);
 #pragma unroll
         for (int u = 0; u < QT; ++u) s[u][k] = mma<T>(kf, qf[u][f], s[u][k]);
       }
-    }
-    if (gaps) {
-#pragma unroll
-      for (int k = 0; k < BK / 16; ++k) {
-        const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + k * 16 + g4 * 4);
+      if constexpr (with_gaps) {
+        const f32x4 b = *reinterpret_cast<const f32x4*>(bb + k * 16 + g4 * 4);
 #pragma unroll
         for (int u = 0; u < QT; ++u)
 #pragma unroll
@@ -244,7 +207,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       }
     }
     bool raise = false;
-    float top[QT];
+    float top[QT], less[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       top[u] = s[u][0][0];
@@ -252,21 +215,22 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       for (int k = 0; k < BK / 16; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top[u] = fmaxf(top[u], s[u][k][r]);
-      raise |= top[u] > far || !met[u];
+      less[u] = 0.f;
+      raise |= top[u] > limit[u];
     }
     if (__any(raise)) {
 #pragma unroll
       for (int u = 0; u < QT; ++u) {
+        const bool met = limit[u] > 0.f;
         const float m = over_lanes16_max(top[u]);  // above the maximum so far
-        const bool up = m > (met[u] ? 0.f : -INFINITY);
-        const float by = up ? m : 0.f, f = met[u] ? exp2_fast(-c * by) : 0.f;
+        const bool up = m > (met ? 0.f : -INFINITY);
+        const float by = up ? m : 0.f, f = met ? exp2_fast(-c * by) : 0.f;
         sum[u] *= f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[u][d] *= f;
-#pragma unroll
-        for (int k = 0; k < BK / 16; ++k) s[u][k] -= by;
+        less[u] = -c * by;
         base[u] -= by;
-        met[u] |= up;
+        limit[u] = up || met ? far : limit[u];
       }
     }
     Piece p[QT][BK / 16 / TILES];
@@ -276,7 +240,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       for (int k = 0; k < BK / 16; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[u][k][r] = exp2_fast(s[u][k][r] * c);
+          s[u][k][r] = exp2_fast(fmaf(s[u][k][r], c, less[u]));
           sum[u][r] += s[u][k][r];
         }
 #pragma unroll
@@ -286,15 +250,28 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int k = 0; k < BK / 16 / TILES; ++k) {
-        const Piece vf = column_piece(vs[buf], LDV, k * 16 * TILES, d * 16, lane);
+        const Piece vf = column_piece(vb, LDV, k * 16 * TILES, d * 16, lane);
 #pragma unroll
         for (int u = 0; u < QT; ++u) o[u][d] = mma<T>(vf, p[u][k], o[u][d]);
       }
+  };
+  for (int32_t t = t0; t < t1; ++t) {
+    const int buf = NB == 1 ? 0 : (t - t0) & 1;
+    if constexpr (NB == 1) wave_sync();
+    kt.put(a, ks[buf], LDK, vs[buf], LDV, bias[buf], tid);
+    if constexpr (NB == 1) wave_sync();
+    else __syncthreads();
+    if (t + 1 < t1) {
+      kt.template fetch<WHOLE>(a, kh, tid);
+      kt.next(a, sk, t + 2, t1, tid);
+    }
+    if (__any(bias[buf][lane % BK] < 0.f)) tile(std::true_type{}, ks[buf], vs[buf], bias[buf]);
+    else                                   tile(std::false_type{}, ks[buf], vs[buf], bias[buf]);
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
     const float total = over_lanes16_sum((sum[u][0] + sum[u][1]) + (sum[u][2] + sum[u][3]));
-    const float top = met[u] ? -c * base[u] : kLowest;
+    const float top = limit[u] > 0.f ? -c * base[u] : kLowest;
     if (q[u].row < 0) continue;
     const int64_t at_row = (int64_t)q[u].row * a.H + q[u].h;
     if (splits > 1) {

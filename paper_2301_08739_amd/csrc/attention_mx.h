@@ -92,7 +92,7 @@ template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T* row,
   }
 }
 
-__device__ const u32x4 kZeroPiece = {0u, 0u, 0u, 0u};
+__device__ u32x4 zero_piece = {0u, 0u, 0u, 0u};  // (never written; a constant would be of another address space, and the loads flat)
 
 // 16 bytes of row `row` (negative: none) and head h from element e on, zero from D on.  WHOLE: rows are pieces of 16 bytes, from their
 // addresses to their ends; what is not there is then read from a piece of zeros, so that a wavefront asks for all its pieces at once.
@@ -100,7 +100,7 @@ template <typename T, bool WHOLE> __device__ __forceinline__ Piece load_piece(co
   Piece p;
   const T* at = row_of_head<const T>(x, row, h) + e;
   if constexpr (WHOLE) {
-    p.q = *(row >= 0 && e < D ? reinterpret_cast<const u32x4*>(at) : &kZeroPiece);
+    p.q = *(row >= 0 && e < D ? reinterpret_cast<const u32x4*>(at) : &zero_piece);
   } else {
     p.q = u32x4{0u, 0u, 0u, 0u};
     if (row < 0) return p;
@@ -218,6 +218,61 @@ template <typename T, int DP, int R, int NT> struct Rows {
   }
 };
 
+// Tiles of BK keys and values on their way into LDS: numbers of rows two tiles ahead, pieces one.  Nothing here waits for what it has
+// just asked for: a row's number is looked at when its piece is asked for, its mask when the piece is put down.
+template <typename T, int DP, int BK, int NT> struct KeyTiles {
+  typedef Rows<T, DP, BK, NT> R;
+  int32_t number[R::U], heads[R::U];
+  Piece k[R::U], v[R::U];
+  uint32_t there;      // bit u: piece u is of a row
+  uint8_t seen[R::U];  // and of one that the mask leaves
+
+  __device__ __forceinline__ void next(const Attn& a, const Span& sk, int32_t t, int32_t end, int tid) {
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      const int r = R::row(tid, u);
+      const int32_t p = t * BK + r;
+      number[u] = t < end && r < BK && p < sk.len ? sk.at + p : -1;
+    }
+    if (a.kl.perm) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u) number[u] = number[u] < 0 ? -1 : a.kl.perm[number[u]];
+    }
+  }
+  template <bool WHOLE> __device__ __forceinline__ void fetch(const Attn& a, int kh, int tid) {
+    there = 0;
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      heads[u] = kh;
+      if ((uint32_t)number[u] >= (uint32_t)a.kl.n) number[u] = -1;
+      there |= number[u] >= 0 ? 1u << u : 0u;
+    }
+    R::template fetch<WHOLE>(k, a.k, number, heads, tid, a.D);
+    R::template fetch<WHOLE>(v, a.v, number, heads, tid, a.D);
+    if (a.mask) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u) seen[u] = number[u] < 0 ? 0 : a.mask[number[u]];
+    }
+  }
+  __device__ __forceinline__ void put(const Attn& a, T* ks, int ldk, T* vs, int ldv, float* bias, int tid) {
+    if (a.mask) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u)
+        if (!seen[u]) {
+          there &= ~(1u << u);
+          k[u].q = v[u].q = u32x4{0u, 0u, 0u, 0u};
+        }
+    }
+    R::put(ks, ldk, k, tid);
+    R::put(vs, ldv, v, tid);
+    if (tid % R::PER == 0) {
+#pragma unroll
+      for (int u = 0; u < R::U; ++u)
+        if (BK * R::PER % NT == 0 || R::row(tid, u) < BK) bias[R::row(tid, u)] = there >> u & 1 ? 0.f : -INFINITY;
+    }
+  }
+};
+
 // A row of queries among those of a group that share their keys: row v is position v / share, head v % share of the key head's
 struct QueryRow {
   int32_t row, h;  // row < 0: none
@@ -229,7 +284,7 @@ __device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int
 
 // May rows of this array be read and written in pieces of 16 bytes?
 inline bool whole_pieces(const Heads& x, int D, size_t size) {
-  return ((uintptr_t)x.p | (uintptr_t)(x.rs * size) | (uintptr_t)(x.hs * size) | (uintptr_t)(D * size)) % 16 == 0;
+  return ((uintptr_t)x.p | (uintptr_t)x.rs | (uintptr_t)x.hs | (uintptr_t)(D * size)) % 16 == 0;
 }
 
 constexpr int kChipWaves = 2048;  // two wavefronts a SIMD

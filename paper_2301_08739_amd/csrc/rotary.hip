@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void k_rotary(Rotary r, RotaryPlan pl) {
     const int c = (int)(in_row - head * pl.head.by);
     const bool key = head >= (uint32_t)r.q_heads;
     const int64_t h = key ? head - r.q_heads : head;
-    const Heads &from = key ? r.k : r.q, &out = key ? r.k_out : r.q_out;
+    const HeadsAt &from = key ? r.k : r.q, &out = key ? r.k_out : r.q_out;
     int e;
     if (c >= pl.turning) {
       e = 2 * turned + (c - pl.turning) * (LOOSE ? 1 : V);
@@ -149,10 +149,10 @@ template <typename T, int V, int S, bool LOOSE = false> int launch(const Rotary&
 template <typename T> int run(const Rotary& r, hipStream_t stream) {
   constexpr int size = (int)sizeof(T), most = 16 / size;
   const int turned = r.axes * r.pairs, rest = r.D - 2 * turned;
-  auto same = [](const Heads& a, const Heads& b) { return a.p == b.p; };
+  auto same = [](const HeadsAt& a, const HeadsAt& b) { return a.p == b.p; };
   const bool copies = rest > 0 && !(same(r.q, r.q_out) && (r.k_heads == 0 || same(r.k, r.k_out)));
   uint64_t all = copies ? (uint64_t)rest * size : 0;
-  for (const Heads* x : {&r.q, &r.q_out, &r.k, &r.k_out})
+  for (const HeadsAt* x : {&r.q, &r.q_out, &r.k, &r.k_out})
     if (x->p) all |= (uintptr_t)x->p | (uint64_t)x->rs * size | (uint64_t)x->hs * size;
   auto fits = [&](int v, int64_t length) { return v <= most && all % (v * size) == 0 && length % v == 0; };
   const int apart = r.layout == FF_ROTARY_INTERLEAVED ? 1 : r.pairs;
