@@ -239,7 +239,7 @@ template <typename T, int DP, bool WHOLE> __global__ __launch_bounds__(256) void
 // dk and dv: NW wavefronts of KW x 16 keys each hold keys, values and the sums of their gradients; the queries that look at them and
 // the gradients of their results go by in tiles of 32 rows through LDS.  splits > 1: each workgroup takes a stretch of the queries.
 template <typename T, int DP, int NW, int KW, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_attention_dkv(Attn a, TileGrid tg, int splits, float* part) {
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_attention_dkv(Attn a, TileGrid tg, Order order, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW, BQ = 32, PQ = 2 / TILES;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T);
   typedef Rows<T, DP, BQ, NT> R;
@@ -248,10 +248,11 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
   __shared__ __attribute__((aligned(16))) T gs[NB][BQ * LD];
   __shared__ __attribute__((aligned(16))) float offs[NB][BQ], deltas[NB][BQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15, share = a.H / a.K;
-  const int split = blockIdx.x % splits;
-  const int32_t rest = blockIdx.x / splits;
-  const int kh = rest / tg.tiles;
-  const TileAt at = tile_at<16 * NW * KW>(a, a.kl, tg, rest - kh * tg.tiles, lane);
+  const uint32_t work = in_order(order);
+  if (work >= order.total) return;
+  const uint32_t row_of_work = work / tg.tiles;
+  const int split = row_of_work / a.K, kh = row_of_work - split * a.K;
+  const TileAt at = tile_at<16 * NW * KW>(a, a.kl, tg, work - row_of_work * tg.tiles, lane);
   if (at.g < 0) return;
   const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
   const int32_t k0 = at.tile * (16 * NW * KW);
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
 // dq: the forward kernel's arrangement, with keys and values by BK through LDS and scores with the keys down (K Q^T), so that e is the
 // right operand of (dq)^T = K^T e^T as it lies in the registers.
 template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(Attn a, TileGrid tg, int splits, float* part) {
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(Attn a, TileGrid tg, Order order, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T), BQ = 16 * QT * NW;
   constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
@@ -420,10 +421,11 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LD];
   __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
-  const int split = blockIdx.x % splits;
-  const int32_t rest = blockIdx.x / splits;
-  const int kh = rest / tg.tiles;
-  const TileAt at = tile_at<BQ>(a, a.ql, tg, rest - kh * tg.tiles, lane);
+  const uint32_t work = in_order(order);
+  if (work >= order.total) return;
+  const uint32_t row_of_work = work / tg.tiles;
+  const int split = row_of_work / a.K, kh = row_of_work - split * a.K;
+  const TileAt at = tile_at<BQ>(a, a.ql, tg, work - row_of_work * tg.tiles, lane);
   if (at.g < 0) return;
   const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
   if ((int64_t)at.tile * BQ >= (int64_t)sq.len * tg.share) return;
@@ -589,7 +591,7 @@ Plan plan(const Attn& a, size_t size) {
   const int64_t gq = (int64_t)p.tq.tiles * a.K, gk = (int64_t)p.tk.tiles * a.K;
   p.splits_q = stretches(gq, p.wide_q ? 4 : 1, a.kl.G);
   p.splits_k = stretches(gk, p.wide_k ? 4 : 1, rows);
-  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX && gk * p.splits_k <= INT32_MAX && ceil_div((int64_t)a.ql.n * a.H, 8) <= INT32_MAX &&
+  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX - 128 && gk * p.splits_k <= INT32_MAX - 128 && ceil_div((int64_t)a.ql.n * a.H, 8) <= INT32_MAX &&
            rows <= INT32_MAX - 64;
   if (p.splits_q > 1) p.fits = p.fits && f[2] && (int64_t)p.sum_q.tiles * a.H <= INT32_MAX;
   if (p.splits_k > 1) p.fits = p.fits && f[3] && (int64_t)p.sum_k.tiles * a.K <= INT32_MAX;
@@ -620,21 +622,23 @@ template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* w
   if (a.ql.n > 0) {
     constexpr int PER = DP * (int)sizeof(T) / 16;
     k_attention_delta<T, DP, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a);
-    const dim3 grid((uint32_t)((int64_t)p.tq.tiles * a.K * p.splits_q));
+    const Order order = make_order((int64_t)p.tq.tiles * a.K * p.splits_q);
+    const uint32_t grid = workgroups(order);
     if (p.wide_q)
-      k_attention_dq<T, DP, 4, 2, 32, WHOLE><<<grid, 256, 0, st>>>(a, p.tq, p.splits_q, pq);
+      k_attention_dq<T, DP, 4, 2, 32, WHOLE><<<grid, 256, 0, st>>>(a, p.tq, order, p.splits_q, pq);
     else
-      k_attention_dq<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tq, p.splits_q, pq);
+      k_attention_dq<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tq, order, p.splits_q, pq);
     if (p.splits_q > 1)
       k_attention_sum<T, DP, 1><<<dim3((uint32_t)ceil_div((int64_t)p.sum_q.tiles * a.H, 4)), 256, 0, st>>>(a, a.ql, p.sum_q, a.H, p.splits_q, pq, a.dq,
                                                                                                        a.dq, a.scale, a.scale);
   }
   if (a.kl.n > 0) {
-    const dim3 grid((uint32_t)((int64_t)p.tk.tiles * a.K * p.splits_k));
+    const Order order = make_order((int64_t)p.tk.tiles * a.K * p.splits_k);
+    const uint32_t grid = workgroups(order);
     if (p.wide_k)
-      k_attention_dkv<T, DP, 4, 2, WHOLE><<<grid, 256, 0, st>>>(a, p.tk, p.splits_k, pk);
+      k_attention_dkv<T, DP, 4, 2, WHOLE><<<grid, 256, 0, st>>>(a, p.tk, order, p.splits_k, pk);
     else
-      k_attention_dkv<T, DP, 1, 1, WHOLE><<<grid, 64, 0, st>>>(a, p.tk, p.splits_k, pk);
+      k_attention_dkv<T, DP, 1, 1, WHOLE><<<grid, 64, 0, st>>>(a, p.tk, order, p.splits_k, pk);
     if (p.splits_k > 1)
       k_attention_sum<T, DP, 2><<<dim3((uint32_t)ceil_div((int64_t)p.sum_k.tiles * a.K, 4)), 256, 0, st>>>(a, a.kl, p.sum_k, a.K, p.splits_k, pk, a.dk,
                                                                                                        a.dv, a.scale, kLower<T>);

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
 // met no key yet, is the maximum made good and what was summed brought down.   Keys that are not there cost something in their own tiles
 // only.  The sum of p is one of float32 additions: a product with ones would sum the rounded p, and lse would be 2^-9 off.
 template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) || (DP == 64 && NW == 4) ? 2 : 1) void k_attention_tiles(Attn a, TileGrid tg, int splits, float* part) {
+__global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) || (DP == 64 && NW == 4) ? 2 : 1) void k_attention_tiles(Attn a, TileGrid tg, Order order, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
   constexpr int KW = NF * KF, LDK = KW + 16 / (int)sizeof(T), LDV = DP + 32 / (int)sizeof(T), BQ = 16 * QT * NW;
   constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
@@ -143,10 +143,11 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LDV];
   __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
-  const int split = blockIdx.x % splits;
-  const int32_t rest = blockIdx.x / splits;
-  const int kh = rest / tg.tiles;
-  const TileAt at = tile_at<BQ>(a, a.ql, tg, rest - kh * tg.tiles, lane);
+  const uint32_t work = in_order(order);
+  if (work >= order.total) return;
+  const uint32_t row_of_work = work / tg.tiles;
+  const int split = row_of_work / a.K, kh = row_of_work - split * a.K;
+  const TileAt at = tile_at<BQ>(a, a.ql, tg, work - row_of_work * tg.tiles, lane);
   if (at.g < 0) return;
   const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
   if ((int64_t)at.tile * BQ >= (int64_t)sq.len * tg.share) return;
@@ -384,7 +385,7 @@ Plan plan(const Attn& a, size_t size) {
   if (s > kMostSplits) s = kMostSplits;
   if (waves * 2 > kChipWaves) s = 1;
   p.splits = (int)s;
-  p.fits = p.fits && groups * s <= INT32_MAX;
+  p.fits = p.fits && groups * s <= INT32_MAX - 128;
   if (s > 1) {
     bool fits;
     p.join = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, 1, &fits);
@@ -410,11 +411,13 @@ template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, 
       return group_launch<T, DP, 8, WHOLE>(a, p, st);
     }
   }
-  const dim3 grid((uint32_t)((int64_t)p.tg.tiles * a.K * p.splits));
+  const Order order = make_order((int64_t)p.tg.tiles * a.K * p.splits);
+  const uint32_t grid = workgroups(order);
+  if (grid == 0) return FF_OK;
   if (p.wide)
-    k_attention_tiles<T, DP, 4, 2, 64, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, p.splits, ws);
+    k_attention_tiles<T, DP, 4, 2, 64, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, order, p.splits, ws);
   else
-    k_attention_tiles<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tg, p.splits, ws);
+    k_attention_tiles<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tg, order, p.splits, ws);
   if (p.splits > 1) k_attention_join<T, DP><<<dim3((uint32_t)((int64_t)p.join.tiles * a.K)), 256, 0, st>>>(a, p.join, p.splits, ws);
   return launch_status();
 }

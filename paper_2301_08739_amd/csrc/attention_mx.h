@@ -200,6 +200,22 @@ inline TileGrid tile_grid(int64_t n, int64_t G, int64_t share, int64_t max_group
   return {(int32_t)(*fits ? tiles : 0), direct ? (int32_t)per : 0, (int32_t)share};
 }
 
+// Workgroups go to the eight XCDs in turn, each with an L2 of its own.  Tiles that read the same rows are neighbours in the order of
+// the work; runs of `run` of them are given to one XCD, as long as that leaves the XCDs evenly filled.
+struct Order {
+  uint32_t total, run;  // workgroups that have work, and of a run
+};
+__device__ __forceinline__ uint32_t in_order(const Order& o) {
+  const uint32_t xcd = blockIdx.x % 8, j = blockIdx.x / 8;
+  return (j / o.run * 8 + xcd) * o.run + j % o.run;
+}
+inline Order make_order(int64_t total) {
+  uint32_t run = 16;
+  while (run > 1 && (total + 8 * run - 1) / (8 * run) * (8 * run) - total > total / 16) run /= 2;
+  return {(uint32_t)total, run};
+}
+inline uint32_t workgroups(const Order& o) { return (o.total + 8 * o.run - 1) / (8 * o.run) * (8 * o.run); }
+
 // ---- a tile of rows into LDS ------------------------------------------------------------------------------
 template <typename T, int DP, int R, int NT> struct Rows {
   static constexpr int PER = DP * (int)sizeof(T) / 16;              // pieces of a row
