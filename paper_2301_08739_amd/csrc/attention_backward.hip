@@ -260,26 +260,28 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
   const int32_t all_rows = sq.len * share, tiles = (all_rows + BQ - 1) / BQ, per = (tiles + splits - 1) / splits;
   const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
+  // As in KeyTiles: numbers two tiles ahead, looked at where their pieces are asked for
   int32_t rows[R::U], heads[R::U];
   auto number = [&](int32_t t) {
+    if (t >= t1) return;
+    const int32_t* const list = a.ql.perm ? a.ql.perm : &zero_number;
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
-      const int r = R::row(tid, u);
-      const int32_t v = t * BQ + r, p = share == 1 ? v : v / share;
-      rows[u] = t < t1 && r < BQ && p < sq.len ? sq.at + p : -1;
-      heads[u] = kh * share + (share == 1 ? 0 : v - p * share);
-    }
-    if (a.ql.perm) {
-#pragma unroll
-      for (int u = 0; u < R::U; ++u) rows[u] = rows[u] < 0 ? -1 : a.ql.perm[rows[u]];
+      const int32_t v = t * BQ + R::row(tid, u), p = share == 1 ? v : v / share;
+      rows[u] = list[a.ql.perm ? sq.at + (p < sq.len ? p : sq.len - 1) : 0];
     }
   };
   Piece qr[R::U], gr[R::U];
   float fo[R::U], fd[R::U];
-  auto fetch = [&]() {  // (numbers are looked at here, not where they are asked for: nothing waits for what it has just asked for)
+  auto fetch = [&](int32_t t) {
 #pragma unroll
-    for (int u = 0; u < R::U; ++u)
-      if ((uint32_t)rows[u] >= (uint32_t)a.ql.n) rows[u] = -1;
+    for (int u = 0; u < R::U; ++u) {
+      const int r = R::row(tid, u);
+      const int32_t v = t * BQ + r, p = share == 1 ? v : v / share;
+      heads[u] = kh * share + (share == 1 ? 0 : v - p * share);
+      if (!a.ql.perm) rows[u] = sq.at + p;
+      if ((uint32_t)rows[u] >= (uint32_t)a.ql.n || p >= sq.len || (BQ * R::PER % NT != 0 && r >= BQ)) rows[u] = -1;
+    }
     R::template fetch<WHOLE>(qr, a.q, rows, heads, tid, a.D);
     R::template fetch<WHOLE>(gr, a.dout, rows, heads, tid, a.D);
 #pragma unroll
@@ -301,7 +303,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
     key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
     live[t] = key[t] >= 0 && (!a.mask || a.mask[key[t]]);
   }
-  fetch();
+  if (t0 < t1) fetch(t0);
   number(t0 + 1);
   Piece kf[KW][NF], vf[KW][NF];
 #pragma unroll
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
     if constexpr (NB == 1) wave_sync();
     else __syncthreads();
     if (t + 1 < t1) {
-      fetch();
+      fetch(t + 1);
       number(t + 2);
     }
     f32x4 s[KW][2], dp[KW][2];
@@ -437,7 +439,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   QueryRow q[QT];
 #pragma unroll
   for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
-  kt.template fetch<WHOLE>(a, kh, tid);
+  if (t0 < t1) kt.template fetch<WHOLE>(a, sk, t0, kh, tid);
   kt.next(a, sk, t0 + 1, t1, tid);
   Piece qf[QT][NF], gf[QT][NF];
   float off[QT], delta[QT];
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
     if constexpr (NB == 1) wave_sync();
     else __syncthreads();
     if (t + 1 < t1) {
-      kt.template fetch<WHOLE>(a, kh, tid);
+      kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
 #pragma unroll

@@ -2,7 +2,6 @@
 // probabilities in registers only.  Scores are computed with the keys down and the queries across (K Q^T), so that a lane holds
 // scores of one query, and the probabilities are the right operand of (out)^T = V^T P^T as they lie in the registers.
 #include "attention_mx.h"
-#include <type_traits>
 
 namespace ff {
 namespace {
@@ -160,7 +159,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   Piece qf[QT][NF];
 #pragma unroll
   for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
-  kt.template fetch<WHOLE>(a, kh, tid);
+  if (t0 < t1) kt.template fetch<WHOLE>(a, sk, t0, kh, tid);
   kt.next(a, sk, t0 + 1, t1, tid);
 #pragma unroll
   for (int u = 0; u < QT; ++u)
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[u][d] = all4(0.f);
   }
-  auto tile = [&](auto with_gaps, const T* kb, const T* vb, const float* bb) {
+  auto tile = [&](bool gaps, const T* kb, const T* vb, const float* bb) {
     f32x4 s[QT][BK / 16];
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k) {
@@ -199,7 +198,10 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
 #pragma unroll
         for (int u = 0; u < QT; ++u) s[u][k] = mma<T>(kf, qf[u][f], s[u][k]);
       }
-      if constexpr (with_gaps) {
+    }
+    if (gaps) {
+#pragma unroll
+      for (int k = 0; k < BK / 16; ++k) {
         const f32x4 b = *reinterpret_cast<const f32x4*>(bb + k * 16 + g4 * 4);
 #pragma unroll
         for (int u = 0; u < QT; ++u)
@@ -263,11 +265,12 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
     if constexpr (NB == 1) wave_sync();
     else __syncthreads();
     if (t + 1 < t1) {
-      kt.template fetch<WHOLE>(a, kh, tid);
+      kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
-    if (__any(bias[buf][lane % BK] < 0.f)) tile(std::true_type{}, ks[buf], vs[buf], bias[buf]);
-    else                                   tile(std::false_type{}, ks[buf], vs[buf], bias[buf]);
+    float worst = bias[buf][lane % BK];
+    if constexpr (BK == 128) worst = fminf(worst, bias[buf][lane + 64]);
+    tile(__any(worst < 0.f), ks[buf], vs[buf], bias[buf]);
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {

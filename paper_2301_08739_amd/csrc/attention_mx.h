@@ -92,6 +92,7 @@ template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T* row,
   }
 }
 
+__device__ int32_t zero_number = 0;
 __device__ u32x4 zero_piece = {0u, 0u, 0u, 0u};  // (never written; a constant would be of another address space, and the loads flat)
 
 // 16 bytes of row `row` (negative: none) and head h from element e on, zero from D on.  WHOLE: rows are pieces of 16 bytes, from their
@@ -243,31 +244,32 @@ template <typename T, int DP, int BK, int NT> struct KeyTiles {
   uint32_t there;      // bit u: piece u is of a row
   uint8_t seen[R::U];  // and of one that the mask leaves
 
+  // Tile t's numbers; end: one behind the last tile there is.  Positions behind the group's end are read as its last.
   __device__ __forceinline__ void next(const Attn& a, const Span& sk, int32_t t, int32_t end, int tid) {
+    if (t >= end) return;
+    const int32_t* const list = a.kl.perm ? a.kl.perm : &zero_number;
+#pragma unroll
+    for (int u = 0; u < R::U; ++u) {
+      const int32_t p = t * BK + R::row(tid, u);
+      number[u] = list[a.kl.perm ? sk.at + (p < sk.len ? p : sk.len - 1) : 0];
+    }
+  }
+  template <bool WHOLE> __device__ __forceinline__ void fetch(const Attn& a, const Span& sk, int32_t t, int kh, int tid) {
+    there = 0;
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
       const int r = R::row(tid, u);
       const int32_t p = t * BK + r;
-      number[u] = t < end && r < BK && p < sk.len ? sk.at + p : -1;
-    }
-    if (a.kl.perm) {
-#pragma unroll
-      for (int u = 0; u < R::U; ++u) number[u] = number[u] < 0 ? -1 : a.kl.perm[number[u]];
-    }
-  }
-  template <bool WHOLE> __device__ __forceinline__ void fetch(const Attn& a, int kh, int tid) {
-    there = 0;
-#pragma unroll
-    for (int u = 0; u < R::U; ++u) {
       heads[u] = kh;
-      if ((uint32_t)number[u] >= (uint32_t)a.kl.n) number[u] = -1;
+      if (!a.kl.perm) number[u] = sk.at + p;
+      if ((uint32_t)number[u] >= (uint32_t)a.kl.n || p >= sk.len || (BK * R::PER % NT != 0 && r >= BK)) number[u] = -1;
       there |= number[u] >= 0 ? 1u << u : 0u;
     }
     R::template fetch<WHOLE>(k, a.k, number, heads, tid, a.D);
     R::template fetch<WHOLE>(v, a.v, number, heads, tid, a.D);
     if (a.mask) {
 #pragma unroll
-      for (int u = 0; u < R::U; ++u) seen[u] = number[u] < 0 ? 0 : a.mask[number[u]];
+      for (int u = 0; u < R::U; ++u) seen[u] = a.mask[number[u] < 0 ? 0 : number[u]];
     }
   }
   __device__ __forceinline__ void put(const Attn& a, T* ks, int ldk, T* vs, int ldv, float* bias, int tid) {
