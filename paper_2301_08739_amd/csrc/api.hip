@@ -113,6 +113,7 @@ int make_attention(const ff_attention_shape* a, int dtype, Attn* out) {
   auto list = [](const ff_group_list& l) { return GroupList{l.perm, l.offsets, (int32_t)l.n, l.G < l.n ? l.G : (l.n ? (int32_t)l.n : 1)}; };
   *out = Attn{};
   out->H = a->heads; out->K = a->kv_heads; out->D = a->head_dim;
+  out->share = make_div(a->heads / a->kv_heads);
   out->scale = a->scale;
   out->num_groups = a->num_groups; out->max_groups = a->max_groups;
   out->ql = list(a->queries); out->kl = list(a->keys);

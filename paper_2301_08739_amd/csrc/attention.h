@@ -14,11 +14,25 @@ struct GroupList {
   const int32_t* off;
   int32_t n, G;
 };
+struct Div {  // quotients of numbers below 2^31 by a constant: a multiplication instead of a division a piece
+  uint32_t by, mul, shift;
+};
+inline Div make_div(uint32_t by) {
+  uint32_t s = 0;
+  while ((1u << s) < by) ++s;
+  const uint64_t m = (((uint64_t)1 << (32 + s)) + by - 1) / by;  // < 2^33: the top bit is added back by hand
+  return {by, (uint32_t)(m - ((uint64_t)1 << 32)), s};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t x, const Div& d) {
+  return d.by == 1 ? x : (uint32_t)(((uint64_t)__umulhi(x, d.mul) + x) >> d.shift);
+}
+
 struct Attn {
   Heads q, k, v, out, dout, dq, dk, dv;
   float* lse;         // [queries, H] or nullptr
-  float* delta;       // [queries, H], workspace of the backward pass
+  float2* stats;      // [queries, H], workspace of the backward pass
   int32_t H, K, D;    // query heads, key heads, elements of a head
+  Div share;          // query heads of a key head
   float scale;
   const int32_t* num_groups;
   int32_t max_groups;

@@ -14,10 +14,23 @@ template <> constexpr float kLift<f16_t> = 12.f;
 template <typename T> constexpr float kLower = 1.f;
 template <> constexpr float kLower<f16_t> = 1.f / 4096.f;
 
-// The logarithm of a row's sum as the exponent's offset: base 2, and +infinity (every p zero) where the row has no key
-template <typename T> __device__ __forceinline__ float as_offset(float lse) {
-  return lse == -INFINITY ? INFINITY : lse * kLog2e - kLift<T>;
+// What the products of a row's scores and of its dp start from: minus the logarithm of the row's sum, in units of the scores
+// (-infinity, every p zero, where the row has no key), and minus delta.  Half precision, whose dp is scaled first: minus delta 2^-12.
+__device__ __forceinline__ float score_start(float lse, float c) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e / c; }
+// p and e, in the places of scores and dp that began so
+template <typename T> __device__ __forceinline__ void p_and_e(f32x4& s, f32x4& dp, float c, f32x4 minus_delta) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if constexpr (kLift<T> > 0.f) {
+      s[r] = exp2_fast(fmaf(s[r], c, kLift<T>));
+      dp[r] = s[r] * fmaf(dp[r], kLower<T>, minus_delta[r]);
+    } else {
+      s[r] = exp2_fast(s[r] * c);
+      dp[r] = s[r] * dp[r];
+    }
+  }
 }
+template <typename T> __device__ __forceinline__ f32x4 dp_start(f32x4 minus_delta) { return kLift<T> > 0.f ? all4(0.f) : minus_delta; }
 
 template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a, const Piece& b) {
   float s = 0.f;
@@ -51,13 +64,12 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
   const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
   T *const et = keys_all[wave], *const qs = rows_all[wave][0], *const gs = rows_all[wave][1];
   float *const offs = stats_all[wave][0], *const deltas = stats_all[wave][1];
-  const int share = a.H / a.K;
   const int64_t item = (int64_t)blockIdx.x * 4 + wave;
   const int kh = (int)(item % a.K);
   if (item / a.K >= groups_of(a)) return;
   const int32_t group = (int32_t)(item / a.K);
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
-  const int32_t rows = sq.len * share;
+  const int32_t rows = sq.len * (int32_t)a.share.by;
 
   int32_t key[RK / 16];
   uint32_t live = 0;  // bit t: key t of this lane is one that queries look at
@@ -93,7 +105,13 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
     for (int x = lane; x < (RK - KT * 16) * LDE / E; x += 64) *reinterpret_cast<u32x4*>(et + KT * 16 * LDE + x * E) = u32x4{0u, 0u, 0u, 0u};
   }
 
-  const float c = a.scale * kLog2e;
+  const float c = exponent_factor(a);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
+  }
   f32x4 dk[KT][DT], dv[KT][DT];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
@@ -106,10 +124,10 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
     float delta[2], off[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      q[u] = query_row(a, sq, share, kh, r0 + u * 16 + i);
+      q[u] = query_row(a, sq, kh, r0 + u * 16 + i);
       delta[u] = 0.f;
-      off[u] = INFINITY;
-      if (q[u].row >= 0) off[u] = as_offset<T>(a.lse[(int64_t)q[u].row * a.H + q[u].h]);
+      off[u] = -INFINITY;
+      if (q[u].row >= 0) off[u] = a.lse[stat_at(a, q[u].row, q[u].h)];
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
@@ -119,9 +137,9 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      delta[u] = over_lanes16_sum(delta[u]) * kLower<T>;
+      delta[u] = over_lanes16_sum(delta[u]) * -kLower<T>;
       if (g4 == 0) {
-        offs[u * 16 + i] = off[u];
+        offs[u * 16 + i] = score_start(off[u], c);
         deltas[u * 16 + i] = delta[u];
       }
 #pragma unroll
@@ -151,17 +169,14 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
       f32x4 s[2], dp[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        s[u] = dp[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        s[u] = fo[u];
+        dp[u] = dp_start<T>(fd[u]);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
           s[u] = mma<T>(qf[u][f], kf[t][f], s[u]);
           dp[u] = mma<T>(gf[u][f], vf[t][f], dp[u]);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[u][r] = exp2_fast(fmaf(s[u][r], c, -fo[u][r]));
-          dp[u][r] = s[u][r] * fmaf(dp[u][r], kLower<T>, -fd[u][r]);
-        }
+        p_and_e<T>(s[u], dp[u], c, fd[u]);
       }
       const bool here = live >> t & 1;
       if (!__all(here)) {  // keys that no query looks at
@@ -221,33 +236,34 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
 }
 
 // ---- any lengths -----------------------------------------------------------------------------------------
-// delta of every row and head: a few lanes a head, 16 bytes each
-template <typename T, int DP, bool WHOLE> __global__ __launch_bounds__(256) void k_attention_delta(Attn a) {
+// What the products of every row and head start from: a few lanes a head, 16 bytes each
+template <typename T, int DP, bool WHOLE> __global__ __launch_bounds__(256) void k_attention_stats(Attn a, Div heads) {
   constexpr int PER = DP * (int)sizeof(T) / 16;
-  const int64_t x = (int64_t)blockIdx.x * (256 / PER) + threadIdx.x / PER, all = (int64_t)a.ql.n * a.H;
+  const uint32_t x = blockIdx.x * (256 / PER) + threadIdx.x / PER, all = (uint32_t)a.ql.n * (uint32_t)a.H;
   const int e = (threadIdx.x % PER) * Mx<T>::E;
-  float s = 0.f;
+  const uint32_t row = quotient(x, heads), h = x - row * heads.by;
+  float s = 0.f, lse = 0.f;
   if (x < all) {
-    const int32_t row = (int32_t)(x / a.H), h = (int32_t)(x % a.H);
+    lse = a.lse[x];
     s = dot_pieces<T>(load_piece<T, WHOLE>(a.dout, row, h, e, a.D), load_piece<T, WHOLE>(a.out, row, h, e, a.D));
   }
 #pragma unroll
   for (int d = PER / 2; d; d >>= 1) s += __shfl_xor(s, d);
-  if (x < all && threadIdx.x % PER == 0) a.delta[x] = s;
+  if (x < all && threadIdx.x % PER == 0) a.stats[x] = make_float2(score_start(lse, exponent_factor(a)), s * -kLower<T>);
 }
 
 // dk and dv: NW wavefronts of KW x 16 keys each hold keys, values and the sums of their gradients; the queries that look at them and
-// the gradients of their results go by in tiles of 32 rows through LDS.  splits > 1: each workgroup takes a stretch of the queries.
-template <typename T, int DP, int NW, int KW, bool WHOLE>
+// the gradients of their results go by in tiles of BQ rows through LDS.  splits > 1: each workgroup takes a stretch of the queries.
+template <typename T, int DP, int NW, int KW, int BQ, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_attention_dkv(Attn a, TileGrid tg, Order order, int splits, float* part) {
-  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW, BQ = 32, PQ = 2 / TILES;
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW, PQ = 2 / TILES;
   constexpr int W = NF * KF, LD = W + 16 / (int)sizeof(T);
   typedef Rows<T, DP, BQ, NT> R;
   constexpr int NB = NW == 1 ? 1 : 2;  // (a wavefront alone writes when it has read)
   __shared__ __attribute__((aligned(16))) T qs[NB][BQ * LD];
   __shared__ __attribute__((aligned(16))) T gs[NB][BQ * LD];
   __shared__ __attribute__((aligned(16))) float offs[NB][BQ], deltas[NB][BQ];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15, share = a.H / a.K;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
   const uint32_t work = in_order(order);
   if (work >= order.total) return;
   const uint32_t row_of_work = work / tg.tiles;
@@ -257,7 +273,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
   const Span sq = span_of(a.ql, at.g), sk = span_of(a.kl, at.g);
   const int32_t k0 = at.tile * (16 * NW * KW);
   if (at.tile > sk.len / (16 * NW * KW) || k0 >= sk.len) return;
-  const int32_t all_rows = sq.len * share, tiles = (all_rows + BQ - 1) / BQ, per = (tiles + splits - 1) / splits;
+  const int32_t all_rows = sq.len * (int32_t)a.share.by, tiles = (all_rows + BQ - 1) / BQ, per = (tiles + splits - 1) / splits;
   const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
   // As in KeyTiles: numbers two tiles ahead, looked at where their pieces are asked for
@@ -267,18 +283,18 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
     const int32_t* const list = a.ql.perm ? a.ql.perm : &zero_number;
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
-      const int32_t v = t * BQ + R::row(tid, u), p = share == 1 ? v : v / share;
+      const int32_t p = quotient(t * BQ + R::row(tid, u), a.share);
       rows[u] = list[a.ql.perm ? sq.at + (p < sq.len ? p : sq.len - 1) : 0];
     }
   };
   Piece qr[R::U], gr[R::U];
-  float fo[R::U], fd[R::U];
+  float2 st[R::U];
   auto fetch = [&](int32_t t) {
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
       const int r = R::row(tid, u);
-      const int32_t v = t * BQ + r, p = share == 1 ? v : v / share;
-      heads[u] = kh * share + (share == 1 ? 0 : v - p * share);
+      const int32_t v = t * BQ + r, p = quotient(v, a.share);
+      heads[u] = kh * a.share.by + v - p * a.share.by;
       if (!a.ql.perm) rows[u] = sq.at + p;
       if ((uint32_t)rows[u] >= (uint32_t)a.ql.n || p >= sq.len || (BQ * R::PER % NT != 0 && r >= BQ)) rows[u] = -1;
     }
@@ -286,12 +302,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
     R::template fetch<WHOLE>(gr, a.dout, rows, heads, tid, a.D);
 #pragma unroll
     for (int u = 0; u < R::U; ++u) {
-      fo[u] = -INFINITY;
-      fd[u] = 0.f;
-      if (tid % R::PER == 0 && rows[u] >= 0) {
-        fo[u] = a.lse[(int64_t)rows[u] * a.H + heads[u]];
-        fd[u] = a.delta[(int64_t)rows[u] * a.H + heads[u]];
-      }
+      st[u] = make_float2(-INFINITY, 0.f);
+      if (tid % R::PER == 0 && rows[u] >= 0) st[u] = a.stats[stat_at(a, rows[u], heads[u])];
     }
   };
   number(t0);
@@ -321,7 +333,13 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
         *reinterpret_cast<u32x4*>(&gs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
       }
   }
-  const float c = a.scale * kLog2e;
+  const float c = exponent_factor(a);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int t = 0; t < KW; ++t)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
+  }
   f32x4 dk[KW][DT], dv[KW][DT];
 #pragma unroll
   for (int t = 0; t < KW; ++t)
@@ -336,8 +354,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
 #pragma unroll
       for (int u = 0; u < R::U; ++u)
         if (BQ * R::PER % NT == 0 || R::row(tid, u) < BQ) {
-          offs[buf][R::row(tid, u)] = as_offset<T>(fo[u]);
-          deltas[buf][R::row(tid, u)] = fd[u] * kLower<T>;
+          offs[buf][R::row(tid, u)] = st[u].x;
+          deltas[buf][R::row(tid, u)] = st[u].y;
         }
     }
     if constexpr (NB == 1) wave_sync();
@@ -346,48 +364,50 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
       fetch(t + 1);
       number(t + 2);
     }
-    f32x4 s[KW][2], dp[KW][2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int half = 0; half < BQ; half += 32) {
+      f32x4 s[KW][2], dp[KW][2];
 #pragma unroll
-      for (int k = 0; k < KW; ++k) s[k][u] = dp[k][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        const Piece qf = row_piece(qs[buf], LD, u * 16 + i, f * KF + g4 * E), gf = row_piece(gs[buf], LD, u * 16 + i, f * KF + g4 * E);
+      for (int u = 0; u < 2; ++u) {
+        const int r = half + u * 16;
+        const f32x4 o = *reinterpret_cast<const f32x4*>(offs[buf] + r + g4 * 4), l = *reinterpret_cast<const f32x4*>(deltas[buf] + r + g4 * 4);
 #pragma unroll
         for (int k = 0; k < KW; ++k) {
-          s[k][u] = mma<T>(qf, kf[k][f], s[k][u]);
-          dp[k][u] = mma<T>(gf, vf[k][f], dp[k][u]);
+          s[k][u] = o;
+          dp[k][u] = dp_start<T>(l);
         }
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const Piece qf = row_piece(qs[buf], LD, r + i, f * KF + g4 * E), gf = row_piece(gs[buf], LD, r + i, f * KF + g4 * E);
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            s[k][u] = mma<T>(qf, kf[k][f], s[k][u]);
+            dp[k][u] = mma<T>(gf, vf[k][f], dp[k][u]);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < KW; ++k) p_and_e<T>(s[k][u], dp[k][u], c, l);
       }
-      const f32x4 o = *reinterpret_cast<const f32x4*>(offs[buf] + u * 16 + g4 * 4), l = *reinterpret_cast<const f32x4*>(deltas[buf] + u * 16 + g4 * 4);
+      Piece p[KW][PQ], e[KW][PQ];
 #pragma unroll
       for (int k = 0; k < KW; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[k][u][r] = exp2_fast(fmaf(s[k][u][r], c, -o[r]));
-          dp[k][u][r] = s[k][u][r] * fmaf(dp[k][u][r], kLower<T>, -l[r]);
+        for (int u = 0; u < PQ; ++u) {
+          p[k][u] = as_piece<T>(s[k] + u * TILES);
+          e[k][u] = as_piece<T>(dp[k] + u * TILES);
+        }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int u = 0; u < PQ; ++u) {
+          const Piece gc = column_piece(gs[buf], LD, half + u * 16 * TILES, d * 16, lane), qc = column_piece(qs[buf], LD, half + u * 16 * TILES, d * 16, lane);
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            dv[k][d] = mma<T>(gc, p[k][u], dv[k][d]);
+            dk[k][d] = mma<T>(qc, e[k][u], dk[k][d]);
+          }
         }
     }
-    Piece p[KW][PQ], e[KW][PQ];
-#pragma unroll
-    for (int k = 0; k < KW; ++k)
-#pragma unroll
-      for (int u = 0; u < PQ; ++u) {
-        p[k][u] = as_piece<T>(s[k] + u * TILES);
-        e[k][u] = as_piece<T>(dp[k] + u * TILES);
-      }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int u = 0; u < PQ; ++u) {
-        const Piece gc = column_piece(gs[buf], LD, u * 16 * TILES, d * 16, lane), qc = column_piece(qs[buf], LD, u * 16 * TILES, d * 16, lane);
-#pragma unroll
-        for (int k = 0; k < KW; ++k) {
-          dv[k][d] = mma<T>(gc, p[k][u], dv[k][d]);
-          dk[k][d] = mma<T>(qc, e[k][u], dk[k][d]);
-        }
-      }
   }
 #pragma unroll
   for (int t = 0; t < KW; ++t) {
@@ -438,23 +458,22 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   kt.next(a, sk, t0, t1, tid);
   QueryRow q[QT];
 #pragma unroll
-  for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
+  for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
   if (t0 < t1) kt.template fetch<WHOLE>(a, sk, t0, kh, tid);
   kt.next(a, sk, t0 + 1, t1, tid);
   Piece qf[QT][NF], gf[QT][NF];
-  float off[QT], delta[QT];
+  f32x4 s0[QT], dp0[QT];
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
-    off[u] = INFINITY;
-    delta[u] = 0.f;
-    if (q[u].row >= 0) {
-      off[u] = as_offset<T>(a.lse[(int64_t)q[u].row * a.H + q[u].h]);
-      delta[u] = a.delta[(int64_t)q[u].row * a.H + q[u].h] * kLower<T>;
-    }
+    float2 st = make_float2(-INFINITY, 0.f);
+    if (q[u].row >= 0) st = a.stats[stat_at(a, q[u].row, q[u].h)];
+    s0[u] = all4(st.x);
+    dp0[u] = all4(st.y);
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
       qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
       gf[u][f] = load_piece<T, WHOLE>(a.dout, q[u].row, q[u].h, f * KF + g4 * E, a.D);
+      if (a.scale < 0.f) qf[u][f] = negated<T>(qf[u][f]);
     }
   }
   if constexpr (W > DP) {
@@ -465,7 +484,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
         *reinterpret_cast<u32x4*>(&vs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
       }
   }
-  const float c = a.scale * kLog2e;
+  const float c = exponent_factor(a);
   f32x4 dq[QT][DT];
 #pragma unroll
   for (int u = 0; u < QT; ++u)
@@ -481,6 +500,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
       kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
+    const bool gaps = __any(bias[buf][lane % BK] < 0.f);
 #pragma unroll
     for (int k = 0; k < BK / 16 / TILES; ++k) {
       f32x4 s[QT][TILES], dp[QT][TILES];
@@ -488,7 +508,10 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
       for (int x = 0; x < TILES; ++x) {
         const int r = (k * TILES + x) * 16;
 #pragma unroll
-        for (int u = 0; u < QT; ++u) s[u][x] = dp[u][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < QT; ++u) {
+          s[u][x] = s0[u];
+          dp[u][x] = dp_start<T>(dp0[u]);
+        }
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
           const Piece kf = row_piece(ks[buf], LD, r + i, f * KF + g4 * E), vf = row_piece(vs[buf], LD, r + i, f * KF + g4 * E);
@@ -498,14 +521,15 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
             dp[u][x] = mma<T>(vf, gf[u][f], dp[u][x]);
           }
         }
-        const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + r + g4 * 4);
+        if (gaps) {
+          const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + r + g4 * 4);
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
+          for (int u = 0; u < QT; ++u)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p = exp2_fast(fmaf(s[u][x][j], c, b[j]) - off[u]);
-            dp[u][x][j] = p * fmaf(dp[u][x][j], kLower<T>, -delta[u]);
-          }
+            for (int j = 0; j < 4; ++j) s[u][x][j] = b[j] < 0.f ? -INFINITY : s[u][x][j];
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u) p_and_e<T>(s[u][x], dp[u][x], c, dp0[u]);
       }
       Piece e[QT];
 #pragma unroll
@@ -523,7 +547,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
     if (q[u].row < 0) continue;
     if (splits > 1) {
       const int64_t all = (int64_t)a.ql.n * a.H;
-      float* to = part + (split * all + (int64_t)q[u].row * a.H + q[u].h) * DP + g4 * 4;
+      float* to = part + (split * all + stat_at(a, q[u].row, q[u].h)) * DP + g4 * 4;
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(to + d * 16) = dq[u][d];
       continue;
@@ -534,73 +558,77 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   }
 }
 
-// Sums of the stretches, a wavefront a row and head; N arrays of DP sums lie side by side in a part.
-template <typename T, int DP, int N>
+// Sums of the stretches, 64 rows of a head a workgroup, four elements a thread; N arrays of DP sums lie side by side in a part.
+template <typename T, int DP, int N, bool WHOLE>
 __global__ __launch_bounds__(256) void k_attention_sum(Attn a, GroupList l, TileGrid tg, int heads, int splits, const float* part, Heads to0, Heads to1,
                                                        float by0, float by1) {
-  const int lane = threadIdx.x & 63;
-  const int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int h = (int)(x / tg.tiles);
-  if (h >= heads) return;
-  const TileAt at = tile_at<1>(a, l, tg, (int32_t)(x - (int64_t)h * tg.tiles), lane);
+  constexpr int LANES = N * DP / 4, ROWS = 64;
+  const int tid = threadIdx.x, h = blockIdx.x / tg.tiles, e = tid % LANES * 4;
+  const TileAt at = tile_at<ROWS>(a, l, tg, blockIdx.x - h * tg.tiles, tid & 63);
   if (at.g < 0) return;
   const Span sp = span_of(l, at.g);
-  const int32_t row = at.tile < sp.len ? row_at(l, sp.at + at.tile) : -1;
-  if (row < 0) return;
-  const int64_t all = (int64_t)l.n * heads * N * DP;
-  part += ((int64_t)row * heads + h) * N * DP;
-  for (int e = lane; e < N * DP; e += 64) {
-    float s = 0.f;
-    for (int k = 0; k < splits; ++k) s += part[k * all + e];
-    const int d = e % DP;
-    if (d < a.D) Elem<T>::store(row_of_head<T>(e < DP ? to0 : to1, row, h) + d, s * (e < DP ? by0 : by1));
+  if (at.tile > sp.len / ROWS) return;
+  const uint64_t all = (uint64_t)(uint32_t)l.n * heads * (N * DP);
+  for (int r = tid / LANES; r < ROWS; r += 256 / LANES) {
+    const int32_t p = at.tile * ROWS + r, row = p < sp.len ? row_at(l, sp.at + p) : -1;
+    if (row < 0) continue;
+    const float* from = part + ((uint64_t)(uint32_t)row * heads + h) * (N * DP) + e;
+    f32x4 s = all4(0.f);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) s += *reinterpret_cast<const f32x4*>(from + k * all);
+    if (N == 1 || e < DP) store4<T, WHOLE>(row_of_head<T>(to0, row, h), e, s * by0, a.D);
+    else                  store4<T, WHOLE>(row_of_head<T>(to1, row, h), e - DP, s * by1, a.D);
   }
 }
 
 // ---- which kernels -----------------------------------------------------------------------------------------
 struct Plan {
   bool group;
-  bool wide_q, wide_k;  // dq: four wavefronts of 32 rows, else one of 16; dkv: four of 32 keys, else one of 16
+  int rows, keys;  // of a workgroup of k_attention_dq: 128 or 16; of k_attention_dkv: 256, 128 or 16
   TileGrid tq, tk, sum_q, sum_k;
   int splits_q, splits_k;
   bool fits;
-  size_t delta, parts_q, parts_k, bytes;  // of the workspace: delta, then the parts of dq, then those of dk and dv
+  size_t stats, parts_q, parts_k, bytes;  // of the workspace: stats, then the parts of dq, then those of dk and dv
 };
-// Stretches of the other side's rows, so that few tiles fill the chip; 256 rows a stretch at least
-int stretches(int64_t groups, int waves, int64_t other) {
-  if (groups < 1 || groups * waves * 2 > kChipWaves) return 1;
-  const int64_t s = ceil_div(kChipWaves, groups * waves), most = other / 256 > 0 ? other / 256 : 1;
+// Stretches of the other side's rows, 256 rows each at least, so that tiles fill the chip; lists of uneven groups twice over, as the
+// tiles of the long groups take longest.  Stretches are paid for with sums in the workspace (2 groups of 4,096 rows, 8 heads of 128
+// elements: 560 us in one, 660 in two; 12 groups of 1 to 4,000 rows: 460 in one, 415 in three).
+int stretches(const TileGrid& tg, int64_t groups, int waves, int64_t other) {
+  const int wanted = tg.per_group.by ? kChipWaves : 2 * kChipWaves;
+  if (groups < 1 || groups * waves >= wanted) return 1;
+  const int64_t s = ceil_div(wanted, groups * waves), most = other / 256 > 0 ? other / 256 : 1;
   return (int)(s < most ? s : most);
 }
 Plan plan(const Attn& a, size_t size) {
   Plan p{};
   const int DP = padded(a.D), share = a.H / a.K;
   const int64_t rows = (int64_t)a.ql.G * share;
-  p.fits = true;
+  p.fits = rows <= INT32_MAX - 512;
+  if (!p.fits) return p;
   p.group = a.kl.G <= 128 && DP <= 32 && rows <= 512;
-  (void)size;
   if (p.group) {
     p.fits = ceil_div((int64_t)a.max_groups * a.K, 4) <= INT32_MAX;
     return p;
   }
   bool f[4];
-  p.wide_q = rows > 32;
-  p.wide_k = a.kl.G > 32;
-  p.tq = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, p.wide_q ? 128 : 16, &f[0]);
-  p.tk = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, p.wide_k ? 128 : 16, &f[1]);
-  p.sum_q = tile_grid(a.ql.n, a.ql.G, 1, a.max_groups, 1, &f[2]);
-  p.sum_k = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, 1, &f[3]);
+  // Few rows go to one wavefront.  Long lists of 16-bit keys of 64 and more elements go by 256 to eight wavefronts, which share what they
+  // read (4,096 keys of 64 elements: 304 us instead of 336, of 128: 650 instead of 720; of groups of 64 keys: 217 instead of 130).
+  p.rows = rows > 32 ? 128 : 16;
+  p.keys = a.kl.G <= 32 ? 16 : size == 2 && DP >= 64 && a.kl.G >= 1024 ? 256 : 128;
+  p.tq = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, p.rows, &f[0]);
+  p.tk = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, p.keys, &f[1]);
+  p.sum_q = tile_grid(a.ql.n, a.ql.G, 1, a.max_groups, 64, &f[2]);
+  p.sum_k = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, 64, &f[3]);
   const int64_t gq = (int64_t)p.tq.tiles * a.K, gk = (int64_t)p.tk.tiles * a.K;
-  p.splits_q = stretches(gq, p.wide_q ? 4 : 1, a.kl.G);
-  p.splits_k = stretches(gk, p.wide_k ? 4 : 1, rows);
-  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX - 128 && gk * p.splits_k <= INT32_MAX - 128 && ceil_div((int64_t)a.ql.n * a.H, 8) <= INT32_MAX &&
-           rows <= INT32_MAX - 64;
+  p.splits_q = stretches(p.tq, gq, p.rows == 16 ? 1 : 4, a.kl.G);
+  p.splits_k = stretches(p.tk, gk, p.keys == 16 ? 1 : p.keys / 32, rows);
+  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX - 128 && gk * p.splits_k <= INT32_MAX - 128 && (int64_t)a.ql.n * a.H <= INT32_MAX;
   if (p.splits_q > 1) p.fits = p.fits && f[2] && (int64_t)p.sum_q.tiles * a.H <= INT32_MAX;
   if (p.splits_k > 1) p.fits = p.fits && f[3] && (int64_t)p.sum_k.tiles * a.K <= INT32_MAX;
-  p.delta = align_up((size_t)a.ql.n * a.H * 4, 256);
+  p.stats = align_up((size_t)a.ql.n * a.H * 8, 256);
   p.parts_q = p.splits_q > 1 ? align_up((size_t)p.splits_q * a.ql.n * a.H * DP * 4, 256) : 0;
   p.parts_k = p.splits_k > 1 ? align_up((size_t)p.splits_k * a.kl.n * a.K * DP * 8, 256) : 0;
-  p.bytes = p.delta + p.parts_q + p.parts_k;
+  p.bytes = p.stats + p.parts_q + p.parts_k;
   return p;
 }
 
@@ -619,30 +647,36 @@ template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* w
       return group_launch<T, DP, 8, WHOLE>(a, st);
     }
   }
-  a.delta = reinterpret_cast<float*>(ws);
-  float *pq = reinterpret_cast<float*>(ws + p.delta), *pk = reinterpret_cast<float*>(ws + p.delta + p.parts_q);
+  // rows of a tile of the other side: fewer barriers, or (float32) fewer registers (64 elements: 16-bit 253 us instead of 272, float32 267
+  // instead of 288)
+  constexpr int BK = sizeof(T) == 2 ? 64 : 32;
+  a.stats = reinterpret_cast<float2*>(ws);
+  float *pq = reinterpret_cast<float*>(ws + p.stats), *pk = reinterpret_cast<float*>(ws + p.stats + p.parts_q);
   if (a.ql.n > 0) {
     constexpr int PER = DP * (int)sizeof(T) / 16;
-    k_attention_delta<T, DP, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a);
+    k_attention_stats<T, DP, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.ql.n * a.H, 256 / PER)), 256, 0, st>>>(a, make_div(a.H));
     const Order order = make_order((int64_t)p.tq.tiles * a.K * p.splits_q);
     const uint32_t grid = workgroups(order);
-    if (p.wide_q)
-      k_attention_dq<T, DP, 4, 2, 32, WHOLE><<<grid, 256, 0, st>>>(a, p.tq, order, p.splits_q, pq);
+    if (p.rows == 128)
+      k_attention_dq<T, DP, 4, 2, BK, WHOLE><<<grid, 256, 0, st>>>(a, p.tq, order, p.splits_q, pq);
     else
       k_attention_dq<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tq, order, p.splits_q, pq);
     if (p.splits_q > 1)
-      k_attention_sum<T, DP, 1><<<dim3((uint32_t)ceil_div((int64_t)p.sum_q.tiles * a.H, 4)), 256, 0, st>>>(a, a.ql, p.sum_q, a.H, p.splits_q, pq, a.dq,
+      k_attention_sum<T, DP, 1, WHOLE><<<dim3((uint32_t)((int64_t)p.sum_q.tiles * a.H)), 256, 0, st>>>(a, a.ql, p.sum_q, a.H, p.splits_q, pq, a.dq,
                                                                                                        a.dq, a.scale, a.scale);
   }
   if (a.kl.n > 0) {
     const Order order = make_order((int64_t)p.tk.tiles * a.K * p.splits_k);
     const uint32_t grid = workgroups(order);
-    if (p.wide_k)
-      k_attention_dkv<T, DP, 4, 2, WHOLE><<<grid, 256, 0, st>>>(a, p.tk, order, p.splits_k, pk);
-    else
-      k_attention_dkv<T, DP, 1, 1, WHOLE><<<grid, 64, 0, st>>>(a, p.tk, order, p.splits_k, pk);
+    if (p.keys == 16) {
+      k_attention_dkv<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tk, order, p.splits_k, pk);
+    } else if (p.keys == 128) {
+      k_attention_dkv<T, DP, 4, 2, BK, WHOLE><<<grid, 256, 0, st>>>(a, p.tk, order, p.splits_k, pk);
+    } else {
+      if constexpr (sizeof(T) == 2 && DP >= 64) k_attention_dkv<T, DP, 8, 2, BK, WHOLE><<<grid, 512, 0, st>>>(a, p.tk, order, p.splits_k, pk);
+    }
     if (p.splits_k > 1)
-      k_attention_sum<T, DP, 2><<<dim3((uint32_t)ceil_div((int64_t)p.sum_k.tiles * a.K, 4)), 256, 0, st>>>(a, a.kl, p.sum_k, a.K, p.splits_k, pk, a.dk,
+      k_attention_sum<T, DP, 2, WHOLE><<<dim3((uint32_t)((int64_t)p.sum_k.tiles * a.K)), 256, 0, st>>>(a, a.kl, p.sum_k, a.K, p.splits_k, pk, a.dk,
                                                                                                        a.dv, a.scale, kLower<T>);
   }
   return launch_status();

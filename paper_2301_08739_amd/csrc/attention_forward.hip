@@ -17,7 +17,6 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
   const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
   T* const vs = vs_all[wave];
   float* const bias = bias_all[wave];
-  const int share = a.H / a.K;
   int64_t item = (int64_t)blockIdx.x * 4 + wave;
   const int kh = (int)(item % a.K);
   item /= a.K;
@@ -26,7 +25,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
   if (item >= groups_of(a)) return;
   const int32_t group = (int32_t)item;
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
-  const int32_t rows = sq.len * share;
+  const int32_t rows = sq.len * (int32_t)a.share.by;
   if (part * 16 >= rows) return;
 
   int32_t key[RK / 16];
@@ -35,7 +34,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
     const int32_t p = t * 16 + i;
     key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
   }
-  QueryRow q = query_row(a, sq, share, kh, part * 16 + i);
+  QueryRow q = query_row(a, sq, kh, part * 16 + i);
   if (a.mask) {
 #pragma unroll
     for (int t = 0; t < RK / 16; ++t)
@@ -82,7 +81,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
 #pragma unroll
       for (int f = 0; f < NF; ++f) s[t] = mma<T>(kf[t][f], qf[f], s[t]);
     if (r0 + parts * 16 < rows) {
-      q = query_row(a, sq, share, kh, r0 + parts * 16 + i);
+      q = query_row(a, sq, kh, r0 + parts * 16 + i);
       fetch_q();
     }
     float top = kLowest;
@@ -119,7 +118,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
     T* out = row_of_head<T>(a.out, now.row, now.h);
 #pragma unroll
     for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
-    if (a.lse && g4 == 0) a.lse[(int64_t)now.row * a.H + now.h] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (a.lse && g4 == 0) a.lse[stat_at(a, now.row, now.h)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
@@ -158,7 +157,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   QueryRow q[QT];
   Piece qf[QT][NF];
 #pragma unroll
-  for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, tg.share, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
+  for (int u = 0; u < QT; ++u) q[u] = query_row(a, sq, kh, at.tile * BQ + (wave * QT + u) * 16 + i);
   if (t0 < t1) kt.template fetch<WHOLE>(a, sk, t0, kh, tid);
   kt.next(a, sk, t0 + 1, t1, tid);
 #pragma unroll
@@ -173,8 +172,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
 #pragma unroll
       for (int e = DP; e < KW; e += E) *reinterpret_cast<u32x4*>(&ks[0][0] + x * LDK + e) = u32x4{0u, 0u, 0u, 0u};
   }
-  // scores as they come from the products grow with the exponents: c > 0 (a scale of zero as next to nothing)
-  const float c = a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e, far = 8.f / c;
+  const float c = exponent_factor(a), far = 8.f / c;
   f32x4 o[QT][DT], sum[QT];
   float base[QT];   // minus the running maximum of the scores
   float limit[QT];  // what a score above it may reach: -infinity until the row has met a key
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
     const float total = over_lanes16_sum((sum[u][0] + sum[u][1]) + (sum[u][2] + sum[u][3]));
     const float top = limit[u] > 0.f ? -c * base[u] : kLowest;
     if (q[u].row < 0) continue;
-    const int64_t at_row = (int64_t)q[u].row * a.H + q[u].h;
+    const int64_t at_row = stat_at(a, q[u].row, q[u].h);
     if (splits > 1) {
       const int64_t all = (int64_t)a.ql.n * a.H;
       float* ml = part + (split * all + at_row) * 2;
@@ -311,9 +309,9 @@ __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int
   const int kh = blockIdx.x / tg.tiles;
   const TileAt at = tile_at<1>(a, a.ql, tg, blockIdx.x - kh * tg.tiles, lane);
   if (at.g < 0) return;
-  const QueryRow q = query_row(a, span_of(a.ql, at.g), tg.share, kh, at.tile);
+  const QueryRow q = query_row(a, span_of(a.ql, at.g), kh, at.tile);
   if (q.row < 0) return;
-  const int64_t all = (int64_t)a.ql.n * a.H, at_row = (int64_t)q.row * a.H + q.h;
+  const int64_t all = (int64_t)a.ql.n * a.H, at_row = stat_at(a, q.row, q.h);
   const float2* const ml = reinterpret_cast<const float2*>(part) + at_row;
   const float* const po = part + splits * all * 2 + at_row * DP + tid % LANES * 4;
   constexpr int MINE = kMostSplits / 256;
@@ -359,7 +357,7 @@ __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int
 struct Plan {
   bool group;       // k_attention_group
   int parts;        // of a group's queries there
-  bool wide;        // k_attention_tiles: four wavefronts of 32 rows, else one of 16
+  int rows;         // of a workgroup of k_attention_tiles: 256, 128 or 16
   TileGrid tg, join;
   int splits;
   bool fits;
@@ -369,7 +367,8 @@ Plan plan(const Attn& a, size_t size) {
   Plan p{};
   const int DP = padded(a.D), share = a.H / a.K;
   const int64_t rows = (int64_t)a.ql.G * share;
-  p.fits = true;
+  p.fits = rows <= INT32_MAX - 512;
+  if (!p.fits) return p;
   p.group = a.kl.G <= 128 && DP <= (size == 4 ? 32 : 64);
   if (p.group) {
     const int64_t waves = (int64_t)a.max_groups * a.K, tiles = ceil_div(rows, 16);
@@ -378,11 +377,18 @@ Plan plan(const Attn& a, size_t size) {
     p.fits = ceil_div(waves * p.parts, 4) <= INT32_MAX;
     return p;
   }
-  p.wide = rows > 32;
-  const int64_t BQ = p.wide ? 128 : 16;
-  p.tg = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, BQ, &p.fits);
-  const int64_t groups = (int64_t)p.tg.tiles * a.K, waves = groups * (p.wide ? 4 : 1);
-  int64_t s = groups ? ceil_div(p.wide ? 2 * kChipWaves : kChipWaves, waves ? waves : 1) : 1;
+  // 128 rows (four wavefronts of 32) unless there are fewer than a third of that.  128 elements of 16 bits, two rounds of the chip and
+  // more: 256 rows, which halves what a thread keeps in flight (4 groups of 4,096 rows, 8 heads: 274 us instead of 311; but 256
+  // workgroups, of 2 groups, 243 instead of 160).
+  auto grid = [&](int r) {
+    p.rows = r;
+    p.tg = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, r, &p.fits);
+    return (int64_t)p.tg.tiles * a.K;
+  };
+  int64_t groups = grid(rows > 32 ? 128 : 16);
+  if (size == 2 && DP == 128 && rows >= 1024 && groups >= 1024) groups = grid(256);
+  const int64_t waves = groups * (p.rows == 16 ? 1 : 4);
+  int64_t s = groups ? ceil_div(p.rows == 16 ? kChipWaves : 2 * kChipWaves, waves ? waves : 1) : 1;
   const int64_t most = a.kl.G / 256 > 0 ? a.kl.G / 256 : 1;
   if (s > most) s = most;
   if (s > kMostSplits) s = kMostSplits;
@@ -417,10 +423,14 @@ template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, 
   const Order order = make_order((int64_t)p.tg.tiles * a.K * p.splits);
   const uint32_t grid = workgroups(order);
   if (grid == 0) return FF_OK;
-  if (p.wide)
-    k_attention_tiles<T, DP, 4, 2, 64, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, order, p.splits, ws);
-  else
+  constexpr int BK = sizeof(T) == 2 && DP <= 32 ? 128 : 64;  // (fewer barriers: 16 elements 106 us instead of 117)
+  if (p.rows == 16) {
     k_attention_tiles<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tg, order, p.splits, ws);
+  } else if (p.rows == 128) {
+    k_attention_tiles<T, DP, 4, 2, BK, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, order, p.splits, ws);
+  } else {
+    if constexpr (sizeof(T) == 2 && DP == 128) k_attention_tiles<T, DP, 8, 2, 64, WHOLE><<<grid, 512, 0, st>>>(a, p.tg, order, p.splits, ws);
+  }
   if (p.splits > 1) k_attention_join<T, DP><<<dim3((uint32_t)((int64_t)p.join.tiles * a.K)), 256, 0, st>>>(a, p.join, p.splits, ws);
   return launch_status();
 }

@@ -164,13 +164,18 @@ __device__ __forceinline__ float over_lanes16_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
+// Scores as they come from the products, as the exponents of p grow with them: c > 0, and the queries (or keys) negated where the
+// scale is negative; a scale of zero as next to nothing.
+__device__ __forceinline__ float exponent_factor(const Attn& a) { return a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e; }
+
 // ---- which tile of which group ---------------------------------------------------------------------------
 // Tiles of B rows (positions times `share` heads that have their keys in common).  Groups of about the same length: tile t is tile
 // t % per_group of group t / per_group.  Else, so that long lists of mostly short groups launch few empty workgroups: group g owns
 // tiles floor(offsets[g] * share / B) + g and on, which is at least as many as it has, whatever the lengths, and a wavefront finds
 // the group of a tile in two or three looks at 64 offsets.
 struct TileGrid {
-  int32_t tiles, per_group, share;  // per_group 0: by offsets
+  int32_t tiles, share;
+  Div per_group;  // by 0: by offsets
 };
 struct TileAt {
   int32_t g, tile;  // g < 0: none
@@ -178,9 +183,9 @@ struct TileAt {
 template <int B> __device__ __forceinline__ TileAt tile_at(const Attn& a, const GroupList& l, const TileGrid& tg, int32_t t, int lane) {
   const int32_t ng = groups_of(a);
   if (ng <= 0) return {-1, 0};
-  if (tg.per_group) {
-    const int32_t g = t / tg.per_group;
-    return {g < ng ? g : -1, t - g * tg.per_group};
+  if (tg.per_group.by) {
+    const int32_t g = quotient(t, tg.per_group);
+    return {g < ng ? g : -1, t - g * (int32_t)tg.per_group.by};
   }
   auto base = [&](int32_t g) { return (int32_t)((int64_t)clamp_to(l.off[g], l.n) * tg.share / B) + g; };
   int32_t lo = 0, hi = ng;
@@ -198,7 +203,7 @@ inline TileGrid tile_grid(int64_t n, int64_t G, int64_t share, int64_t max_group
   const bool direct = even <= by_offsets + by_offsets / 2;
   const int64_t tiles = direct ? even : by_offsets;
   *fits = tiles <= INT32_MAX;
-  return {(int32_t)(*fits ? tiles : 0), direct ? (int32_t)per : 0, (int32_t)share};
+  return {(int32_t)(*fits ? tiles : 0), (int32_t)share, direct && *fits && per > 0 ? make_div((uint32_t)per) : Div{0, 0, 0}};
 }
 
 // Workgroups go to the eight XCDs in turn, each with an L2 of its own.  Tiles that read the same rows are neighbours in the order of
@@ -295,10 +300,11 @@ template <typename T, int DP, int BK, int NT> struct KeyTiles {
 struct QueryRow {
   int32_t row, h;  // row < 0: none
 };
-__device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int share, int kh, int32_t v) {
-  const int32_t p = share == 1 ? v : v / share, h = kh * share + (share == 1 ? 0 : v - p * share);
+__device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int kh, int32_t v) {
+  const int32_t p = quotient(v, a.share), h = kh * a.share.by + v - p * a.share.by;
   return {p < sq.len ? row_at(a.ql, sq.at + p) : -1, h};
 }
+__device__ __forceinline__ uint64_t stat_at(const Attn& a, int32_t row, int32_t h) { return (uint64_t)(uint32_t)row * (uint32_t)a.H + (uint32_t)h; }
 
 // May rows of this array be read and written in pieces of 16 bytes?
 inline bool whole_pieces(const Heads& x, int D, size_t size) {

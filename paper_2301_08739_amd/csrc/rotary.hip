@@ -6,19 +6,6 @@
 namespace ff {
 namespace {
 
-struct Div {  // quotients of numbers below 2^31 by a constant: a multiplication instead of a division a piece
-  uint32_t by, mul, shift;
-};
-Div make_div(uint32_t by) {
-  uint32_t s = 0;
-  while ((1u << s) < by) ++s;
-  const uint64_t m = (((uint64_t)1 << (32 + s)) + by - 1) / by;  // < 2^33: the top bit is added back by hand
-  return {by, (uint32_t)(m - ((uint64_t)1 << 32)), s};
-}
-__device__ __forceinline__ uint32_t quotient(uint32_t x, const Div& d) {
-  return d.by == 1 ? x : (uint32_t)(((uint64_t)__umulhi(x, d.mul) + x) >> d.shift);
-}
-
 constexpr int kPieces = 4;             // of a thread, all in flight together
 constexpr int kItems = 256 * kPieces;  // of a workgroup
 constexpr int kAngles = 2048;          // sines and cosines of a workgroup
