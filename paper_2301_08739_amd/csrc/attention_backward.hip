@@ -52,35 +52,41 @@ template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a
 // ---- short groups: a wavefront holds all keys, values and their gradients of a group and key head ---------------
 // Scores with the queries down and the keys across (Q K^T): a lane holds scores of one key, and p and e are the right operands of
 // (dv)^T = dout^T p and (dk)^T = q^T e as they lie in the registers.  For (dq)^T = K^T e^T e goes through LDS once, which turns it.
-// Queries by 32, delta from their own rows on the way.
+// Queries by 16, delta from their own rows on the way.
 template <typename T, int DP, int KT, bool WHOLE>
-__global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1) void k_attention_backward_group(Attn a) {
-  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, PQ = 2 / TILES;
-  constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 32 + PAD;
+__global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1) void k_attention_backward_group(Attn a, Items items) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16;
+  constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 16 + PAD;
   constexpr int PER = DP * (int)sizeof(T) / 16;
   __shared__ __attribute__((aligned(16))) T keys_all[4][RK * (LD > LDE ? LD : LDE)];  // keys, then e
-  __shared__ __attribute__((aligned(16))) T rows_all[4][2][32 * LD];                  // q and dout
-  __shared__ __attribute__((aligned(16))) float stats_all[4][2][32];
-  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+  __shared__ __attribute__((aligned(16))) T rows_all[4][2][16 * LD];                  // q and dout
+  __shared__ __attribute__((aligned(16))) float stats_all[4][2][16];
+  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   T *const et = keys_all[wave], *const qs = rows_all[wave][0], *const gs = rows_all[wave][1];
   float *const offs = stats_all[wave][0], *const deltas = stats_all[wave][1];
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  const int kh = (int)(item % a.K);
-  if (item / a.K >= groups_of(a)) return;
-  const int32_t group = (int32_t)(item / a.K);
+  const uint32_t item = blockIdx.x * 4 + wave;
+  if (item >= items.total) return;
+  const uint32_t group = quotient(item, items.heads);
+  const int kh = item - group * items.heads.by;
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
   const int32_t rows = sq.len * (int32_t)a.share.by;
+  if ((int32_t)group >= groups_of(a)) return;
 
   int32_t key[RK / 16];
   uint32_t live = 0;  // bit t: key t of this lane is one that queries look at
+  QueryTiles qt;
+  if (rows > 0) qt.ask(a, sq, i);
+  key_rows(key, a, sk, i);
+  if (a.mask) {
+    uint8_t seen[RK / 16];
 #pragma unroll
-  for (int t = 0; t < RK / 16; ++t) {
-    const int32_t p = t * 16 + i;
-    key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
+    for (int t = 0; t < RK / 16; ++t) seen[t] = key[t] < 0 ? 0 : a.mask[key[t]];
+#pragma unroll
+    for (int t = 0; t < RK / 16; ++t) live |= seen[t] ? 1u << t : 0u;
+  } else {
+#pragma unroll
+    for (int t = 0; t < RK / 16; ++t) live |= key[t] >= 0 ? 1u << t : 0u;
   }
-#pragma unroll
-  for (int t = 0; t < RK / 16; ++t)
-    if (key[t] >= 0 && (!a.mask || a.mask[key[t]])) live |= 1u << t;
   Piece kf[KT][NF], vf[KT][NF];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
@@ -89,6 +95,22 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
       kf[t][f] = load_piece<T, WHOLE>(a.k, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
       vf[t][f] = load_piece<T, WHOLE>(a.v, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
     }
+  // The rows of the next sixteen queries are on their way while these are worked on, and their numbers before them
+  QueryRow q;
+  Piece qf[NF], gf[NF], of[NF];
+  float lse;
+  auto fetch = [&](int32_t r0) {
+    q = qt.row(a, sq, kh, r0 + i);
+    qt.ask(a, sq, r0 + 16 + i);
+    lse = q.row >= 0 ? a.lse[stat_at(a, q.row, q.h)] : -INFINITY;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
+      gf[f] = load_piece<T, WHOLE>(a.dout, q.row, q.h, f * KF + g4 * E, a.D);
+      of[f] = load_piece<T, WHOLE>(a.out, q.row, q.h, f * KF + g4 * E, a.D);
+    }
+  };
+  if (rows > 0) fetch(0);
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t)
 #pragma unroll
@@ -118,106 +140,71 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  for (int32_t r0 = 0; r0 < rows; r0 += 32) {
-    QueryRow q[2];
-    Piece qf[2][NF], gf[2][NF];
-    float delta[2], off[2];
+  for (int32_t r0 = 0; r0 < rows; r0 += 16) {
+    float delta = 0.f;
+    Piece qr[NF], gr[NF];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      q[u] = query_row(a, sq, kh, r0 + u * 16 + i);
-      delta[u] = 0.f;
-      off[u] = -INFINITY;
-      if (q[u].row >= 0) off[u] = a.lse[stat_at(a, q[u].row, q[u].h)];
-#pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        qf[u][f] = load_piece<T, WHOLE>(a.q, q[u].row, q[u].h, f * KF + g4 * E, a.D);
-        gf[u][f] = load_piece<T, WHOLE>(a.dout, q[u].row, q[u].h, f * KF + g4 * E, a.D);
-        delta[u] += dot_pieces<T>(gf[u][f], load_piece<T, WHOLE>(a.out, q[u].row, q[u].h, f * KF + g4 * E, a.D));
+    for (int f = 0; f < NF; ++f) {
+      qr[f] = qf[f];
+      gr[f] = gf[f];
+      delta += dot_pieces<T>(gf[f], of[f]);
+      if (f * 4 + g4 < PER) {
+        *reinterpret_cast<u32x4*>(qs + i * LD + f * KF + g4 * E) = qf[f].q;
+        *reinterpret_cast<u32x4*>(gs + i * LD + f * KF + g4 * E) = gf[f].q;
       }
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      delta[u] = over_lanes16_sum(delta[u]) * -kLower<T>;
-      if (g4 == 0) {
-        offs[u * 16 + i] = score_start(off[u], c);
-        deltas[u * 16 + i] = delta[u];
-      }
-#pragma unroll
-      for (int f = 0; f < NF; ++f)
-        if (f * 4 + g4 < PER) {
-          *reinterpret_cast<u32x4*>(qs + (u * 16 + i) * LD + f * KF + g4 * E) = qf[u][f].q;
-          *reinterpret_cast<u32x4*>(gs + (u * 16 + i) * LD + f * KF + g4 * E) = gf[u][f].q;
-        }
+    delta = over_lanes16_sum(delta) * -kLower<T>;
+    if (g4 == 0) {
+      offs[i] = score_start(lse, c);
+      deltas[i] = delta;
     }
+    const QueryRow now = q;
+    if (r0 + 16 < rows) fetch(r0 + 16);
     wave_sync();
-    f32x4 fo[2], fd[2];
+    const f32x4 fo = *reinterpret_cast<const f32x4*>(offs + g4 * 4), fd = *reinterpret_cast<const f32x4*>(deltas + g4 * 4);
+    Piece qc[DT], gc[DT];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      fo[u] = *reinterpret_cast<const f32x4*>(offs + u * 16 + g4 * 4);
-      fd[u] = *reinterpret_cast<const f32x4*>(deltas + u * 16 + g4 * 4);
+    for (int d = 0; d < DT; ++d) {
+      qc[d] = column_half(qs, LD, 0, d * 16, lane);
+      gc[d] = column_half(gs, LD, 0, d * 16, lane);
     }
-    Piece qc[DT][PQ], gc[DT][PQ];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int u = 0; u < PQ; ++u) {
-        qc[d][u] = column_piece(qs, LD, u * 16 * TILES, d * 16, lane);
-        gc[d][u] = column_piece(gs, LD, u * 16 * TILES, d * 16, lane);
-      }
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      f32x4 s[2], dp[2];
+      f32x4 s = fo, dp = dp_start<T>(fd);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        s[u] = fo[u];
-        dp[u] = dp_start<T>(fd[u]);
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          s[u] = mma<T>(qf[u][f], kf[t][f], s[u]);
-          dp[u] = mma<T>(gf[u][f], vf[t][f], dp[u]);
-        }
-        p_and_e<T>(s[u], dp[u], c, fd[u]);
+      for (int f = 0; f < NF; ++f) {
+        s = mma<T>(qr[f], kf[t][f], s);
+        dp = mma<T>(gr[f], vf[t][f], dp);
       }
+      p_and_e<T>(s, dp, c, fd);
       const bool here = live >> t & 1;
       if (!__all(here)) {  // keys that no query looks at
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) dp[u][r] = here ? dp[u][r] : 0.f;
+        for (int r = 0; r < 4; ++r) dp[r] = here ? dp[r] : 0.f;
       }
+      const Piece p = as_half<T>(s), e = as_half<T>(dp);
 #pragma unroll
-      for (int u = 0; u < PQ; ++u) {
-        const Piece p = as_piece<T>(s + u * TILES), e = as_piece<T>(dp + u * TILES);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          dv[t][d] = mma<T>(gc[d][u], p, dv[t][d]);
-          dk[t][d] = mma<T>(qc[d][u], e, dk[t][d]);
-        }
-        if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LDE + u * 16 + g4 * 4) = e.q;
-        } else {
-          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.s[0];
-          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + 16 + g4 * 4) = e.s[1];
-        }
+      for (int d = 0; d < DT; ++d) {
+        dv[t][d] = mma_half<T>(gc[d], p, dv[t][d]);
+        dk[t][d] = mma_half<T>(qc[d], e, dk[t][d]);
       }
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.q;
+      else                          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.s[0];
     }
     wave_sync();
+    f32x4 dq[DT];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x4 dq[DT];
+    for (int d = 0; d < DT; ++d) dq[d] = all4(0.f);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) dq[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < KP; ++t) {
+      const Piece e = column_piece(et, LDE, t * 16 * TILES, 0, lane);
 #pragma unroll
-      for (int t = 0; t < KP; ++t) {
-        const Piece e = column_piece(et, LDE, t * 16 * TILES, u * 16, lane);
+      for (int d = 0; d < DT; ++d) dq[d] = mma<T>(kc[d][t], e, dq[d]);
+    }
+    if (now.row >= 0) {
+      T* to = row_of_head<T>(a.dq, now.row, now.h);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) dq[d] = mma<T>(kc[d][t], e, dq[d]);
-      }
-      if (q[u].row >= 0) {
-        T* to = row_of_head<T>(a.dq, q[u].row, q[u].h);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) store4<T, WHOLE>(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D);
-      }
+      for (int d = 0; d < DT; ++d) store4<T, WHOLE>(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D);
     }
     wave_sync();
   }
@@ -599,15 +586,17 @@ int stretches(const TileGrid& tg, int64_t groups, int waves, int64_t other) {
   const int64_t s = ceil_div(wanted, groups * waves), most = other / 256 > 0 ? other / 256 : 1;
   return (int)(s < most ? s : most);
 }
+// Does a wavefront have registers for the keys and values of a group, and for their gradients?
+constexpr bool holds_group(int DP, int64_t G, size_t size) { return DP <= 32 && G <= 128 && (size == 2 || (G + 15) / 16 * DP <= 160); }
 Plan plan(const Attn& a, size_t size) {
   Plan p{};
   const int DP = padded(a.D), share = a.H / a.K;
   const int64_t rows = (int64_t)a.ql.G * share;
   p.fits = rows <= INT32_MAX - 512;
   if (!p.fits) return p;
-  p.group = a.kl.G <= 128 && DP <= 32 && rows <= 512;
+  p.group = holds_group(DP, a.kl.G, size) && rows <= 512;
   if (p.group) {
-    p.fits = ceil_div((int64_t)a.max_groups * a.K, 4) <= INT32_MAX;
+    p.fits = (int64_t)a.max_groups * a.K <= INT32_MAX;
     return p;
   }
   bool f[4];
@@ -633,7 +622,8 @@ Plan plan(const Attn& a, size_t size) {
 }
 
 template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, hipStream_t st) {
-  k_attention_backward_group<T, DP, KT, WHOLE><<<dim3((uint32_t)ceil_div((int64_t)a.max_groups * a.K, 4)), 256, 0, st>>>(a);
+  const Items items = make_items(a.max_groups, a.K, 1);
+  k_attention_backward_group<T, DP, KT, WHOLE><<<(items.total + 3) / 4, 256, 0, st>>>(a, items);
   return launch_status();
 }
 template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* ws, hipStream_t st) {
@@ -643,8 +633,10 @@ template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* w
       if (kt <= 2) return group_launch<T, DP, 2, WHOLE>(a, st);
       if (kt <= 4) return group_launch<T, DP, 4, WHOLE>(a, st);
       if (kt <= 5) return group_launch<T, DP, 5, WHOLE>(a, st);
-      if (kt <= 6) return group_launch<T, DP, 6, WHOLE>(a, st);
-      return group_launch<T, DP, 8, WHOLE>(a, st);
+      if constexpr (holds_group(DP, 128, sizeof(T))) {
+        if (kt <= 6) return group_launch<T, DP, 6, WHOLE>(a, st);
+        return group_launch<T, DP, 8, WHOLE>(a, st);
+      }
     }
   }
   // rows of a tile of the other side: fewer barriers, or (float32) fewer registers (64 elements: 16-bit 253 us instead of 272, float32 267

@@ -9,53 +9,55 @@ namespace {
 // ---- short groups: a wavefront holds all keys and values of a group and head ----------------------------------
 // Keys and values are read once into registers (values through LDS, which turns them), the queries go by 16 at a time.
 template <typename T, int DP, int KT, bool WHOLE>
-__global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, int parts) {
+__global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, Items items) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16;
   constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, LD = DP + 16 / (int)sizeof(T), PER = DP * (int)sizeof(T) / 16;
   __shared__ __attribute__((aligned(16))) T vs_all[4][RK * LD];
   __shared__ __attribute__((aligned(16))) float bias_all[4][RK];
-  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   T* const vs = vs_all[wave];
   float* const bias = bias_all[wave];
-  int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  const int kh = (int)(item % a.K);
-  item /= a.K;
-  const int part = (int)(item % parts);
-  item /= parts;
-  if (item >= groups_of(a)) return;
-  const int32_t group = (int32_t)item;
+  const uint32_t item = blockIdx.x * 4 + wave;
+  if (item >= items.total) return;
+  const uint32_t rest = quotient(item, items.heads), group = quotient(rest, items.parts);
+  const int kh = item - rest * items.heads.by;
+  const int32_t step = 16 * items.parts.by, first = 16 * (rest - group * items.parts.by);
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
   const int32_t rows = sq.len * (int32_t)a.share.by;
-  if (part * 16 >= rows) return;
+  if ((int32_t)group >= groups_of(a) || first >= rows) return;
 
   int32_t key[RK / 16];
-#pragma unroll
-  for (int t = 0; t < RK / 16; ++t) {
-    const int32_t p = t * 16 + i;
-    key[t] = p < sk.len ? row_at(a.kl, sk.at + p) : -1;
-  }
-  QueryRow q = query_row(a, sq, kh, part * 16 + i);
+  QueryTiles qt;
+  qt.ask(a, sq, first + i);
+  key_rows(key, a, sk, i);
+  QueryRow q = qt.row(a, sq, kh, first + i);
+  qt.ask(a, sq, first + step + i);
   if (a.mask) {
+    uint8_t seen[RK / 16];
+#pragma unroll
+    for (int t = 0; t < RK / 16; ++t) seen[t] = key[t] < 0 ? 0 : a.mask[key[t]];
 #pragma unroll
     for (int t = 0; t < RK / 16; ++t)
-      if (key[t] >= 0 && !a.mask[key[t]]) key[t] = -1;
+      if (!seen[t]) key[t] = -1;
   }
   Piece kf[KT][NF], vr[RK / 16][(PER + 3) / 4], qf[NF];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int f = 0; f < NF; ++f) kf[t][f] = load_piece<T, WHOLE>(a.k, key[t], kh, f * KF + g4 * E, a.D);
-  auto fetch_q = [&]() {
 #pragma unroll
-    for (int f = 0; f < NF; ++f) qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
-  };
-  fetch_q();
+  for (int f = 0; f < NF; ++f) qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t)
 #pragma unroll
-    for (int c = 0; c < (PER + 3) / 4; ++c) {
-      vr[t][c] = load_piece<T, WHOLE>(a.v, key[t], kh, (c * 4 + g4) * E, a.D);
-    }
+    for (int c = 0; c < (PER + 3) / 4; ++c) vr[t][c] = load_piece<T, WHOLE>(a.v, key[t], kh, (c * 4 + g4) * E, a.D);
+  const float c = exponent_factor(a);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
+  }
 #pragma unroll
   for (int t = 0; t < RK / 16; ++t) {
 #pragma unroll
@@ -70,55 +72,54 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
 #pragma unroll
     for (int t = 0; t < KP; ++t) vf[d][t] = column_piece(vs, LD, t * 16 * TILES, d * 16, lane);
 
-  const float c = a.scale * kLog2e;
-  for (int32_t r0 = part * 16; r0 < rows; r0 += parts * 16) {
-    const QueryRow now = q;
+  for (int32_t r0 = first; r0 < rows; r0 += step) {
+    const QueryRow next = qt.row(a, sq, kh, r0 + step + i);
+    Piece qn[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qn[f] = load_piece<T, WHOLE>(a.q, next.row, next.h, f * KF + g4 * E, a.D);
+    qt.ask(a, sq, r0 + 2 * step + i);
     f32x4 s[KP * TILES];
 #pragma unroll
-    for (int t = 0; t < KP * TILES; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < KP * TILES; ++t) s[t] = t < KT ? *reinterpret_cast<const f32x4*>(bias + t * 16 + g4 * 4) : all4(0.f);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int f = 0; f < NF; ++f) s[t] = mma<T>(kf[t][f], qf[f], s[t]);
-    if (r0 + parts * 16 < rows) {
-      q = query_row(a, sq, kh, r0 + parts * 16 + i);
-      fetch_q();
-    }
     float top = kLowest;
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const f32x4 b = *reinterpret_cast<const f32x4*>(bias + t * 16 + g4 * 4);
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[t][r] = fmaf(s[t][r], c, b[r]);
-        top = fmaxf(top, s[t][r]);
-      }
-    }
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
     top = over_lanes16_max(top);
+    top = top > kLowest ? top * c : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[t][r] = exp2_fast(s[t][r] - top);
+        s[t][r] = exp2_fast(fmaf(s[t][r], c, -top));
         sum += s[t][r];
       }
     sum = over_lanes16_sum(sum);
     f32x4 o[DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; ++d) o[d] = all4(0.f);
 #pragma unroll
     for (int t = 0; t < KP; ++t) {
       const Piece p = as_piece<T>(s + t * TILES);
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] = mma<T>(vf[d][t], p, o[d]);
     }
-    if (now.row < 0) continue;
-    const float by = sum == 0.f ? 0.f : 1.f / sum;  // no key: zero
-    T* out = row_of_head<T>(a.out, now.row, now.h);
+    if (q.row >= 0) {
+      const float by = sum == 0.f ? 0.f : 1.f / sum;  // no key: zero
+      T* out = row_of_head<T>(a.out, q.row, q.h);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
-    if (a.lse && g4 == 0) a.lse[stat_at(a, now.row, now.h)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+      for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
+      if (a.lse && g4 == 0) a.lse[stat_at(a, q.row, q.h)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+    q = next;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qf[f] = qn[f];
   }
 }
 
@@ -374,7 +375,7 @@ Plan plan(const Attn& a, size_t size) {
     const int64_t waves = (int64_t)a.max_groups * a.K, tiles = ceil_div(rows, 16);
     const int64_t want = waves ? ceil_div(kChipWaves, waves) : 1;
     p.parts = (int)(want < tiles ? want : tiles);
-    p.fits = ceil_div(waves * p.parts, 4) <= INT32_MAX;
+    p.fits = waves * p.parts <= INT32_MAX;
     return p;
   }
   // 128 rows (four wavefronts of 32) unless there are fewer than a third of that.  128 elements of 16 bits, two rounds of the chip and
@@ -405,8 +406,8 @@ Plan plan(const Attn& a, size_t size) {
 }
 
 template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, const Plan& p, hipStream_t st) {
-  const int64_t waves = (int64_t)a.max_groups * a.K * p.parts;
-  k_attention_group<T, DP, KT, WHOLE><<<dim3((uint32_t)ceil_div(waves, 4)), 256, 0, st>>>(a, p.parts);
+  const Items items = make_items(a.max_groups, a.K, p.parts);
+  k_attention_group<T, DP, KT, WHOLE><<<(items.total + 3) / 4, 256, 0, st>>>(a, items);
   return launch_status();
 }
 template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, float* ws, hipStream_t st) {

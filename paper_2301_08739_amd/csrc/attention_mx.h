@@ -74,6 +74,20 @@ template <> __device__ __forceinline__ Piece as_piece<float>(const f32x4* t) {
   return p;
 }
 
+// The same for one result tile of sixteen rows, where that is all a product sums over (16 bits: half a piece, s[0])
+template <typename T> __device__ __forceinline__ Piece as_half(f32x4 t) {
+  const f32x4 both[2] = {t, t};
+  return as_piece<T>(both);
+}
+template <typename T> __device__ __forceinline__ f32x4 mma_half(const Piece& a, const Piece& b, f32x4 c);
+template <> __device__ __forceinline__ f32x4 mma_half<bf16_t>(const Piece& a, const Piece& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a.s[0], b.s[0], c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 mma_half<f16_t>(const Piece& a, const Piece& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16f16(a.h4[0], b.h4[0], c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x4 mma_half<float>(const Piece& a, const Piece& b, f32x4 c) { return mma<float>(a, b, c); }
+
 // Four elements side by side (one lane's part of a result tile) into memory, those from D on left out
 template <typename T, bool WHOLE> __device__ __forceinline__ void store4(T* row, int e, f32x4 v, int D) {
   if constexpr (WHOLE) {
@@ -133,6 +147,17 @@ template <typename T> __device__ __forceinline__ Piece column_piece(const T* til
     p.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * ld));
   }
   return p;
+}
+// and the half of it for sixteen rows
+template <typename T> __device__ __forceinline__ Piece column_half(const T* tile, int ld, int r0, int d0, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    return column_piece(tile, ld, r0, d0, lane);
+  } else {
+    Piece p;
+    const int g = lane >> 4, i = lane & 15;
+    p.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (r0 + 4 * g + (i >> 2)) * ld + d0 + (i & 3) * 4));
+    return p;
+  }
 }
 template <typename T> __device__ __forceinline__ Piece row_piece(const T* tile, int ld, int r, int e) {
   Piece p;
@@ -305,6 +330,47 @@ __device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int
   return {p < sq.len ? row_at(a.ql, sq.at + p) : -1, h};
 }
 __device__ __forceinline__ uint64_t stat_at(const Attn& a, int32_t row, int32_t h) { return (uint64_t)(uint32_t)row * (uint32_t)a.H + (uint32_t)h; }
+
+// Rows of queries on their way to a wavefront that goes through a group's, 16 a tile: a tile's numbers are asked for two tiles before
+// it, and looked at a tile before it.
+struct QueryTiles {
+  int32_t raw;  // number of this lane's row in the next tile but one
+  __device__ __forceinline__ void ask(const Attn& a, const Span& sq, int32_t v) {
+    const int32_t* const list = a.ql.perm ? a.ql.perm : &zero_number;
+    const int32_t p = quotient(v, a.share);
+    raw = list[a.ql.perm ? sq.at + (p < sq.len ? p : sq.len - 1) : 0];
+  }
+  __device__ __forceinline__ QueryRow row(const Attn& a, const Span& sq, int kh, int32_t v) const {
+    const int32_t p = quotient(v, a.share), r = a.ql.perm ? raw : sq.at + p;
+    return {p < sq.len && (uint32_t)r < (uint32_t)a.ql.n ? r : -1, (int32_t)(kh * a.share.by + v - p * a.share.by)};
+  }
+};
+// Rows of the first N x 16 keys of a group, this lane's of each sixteen; asked for together.
+template <int N> __device__ __forceinline__ void key_rows(int32_t (&key)[N], const Attn& a, const Span& sk, int i) {
+  if (sk.len <= 0) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) key[t] = -1;
+    return;
+  }
+  const int32_t* const list = a.kl.perm ? a.kl.perm : &zero_number;
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const int32_t p = t * 16 + i;
+    key[t] = list[a.kl.perm ? sk.at + (p < sk.len ? p : sk.len - 1) : 0];
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const int32_t p = t * 16 + i;
+    if (!a.kl.perm) key[t] = sk.at + p;
+    if (p >= sk.len || (uint32_t)key[t] >= (uint32_t)a.kl.n) key[t] = -1;
+  }
+}
+// Which of a launch's wavefronts this is: heads side by side, then parts of a group's queries, then groups
+struct Items {
+  uint32_t total;
+  Div heads, parts;
+};
+inline Items make_items(int64_t groups, int heads, int parts) { return {(uint32_t)(groups * heads * parts), make_div(heads), make_div(parts)}; }
 
 // May rows of this array be read and written in pieces of 16 bytes?
 inline bool whole_pieces(const Heads& x, int D, size_t size) {
