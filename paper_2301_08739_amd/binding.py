@@ -468,9 +468,9 @@ def _refuse(what, why):
 
 
 def _heads(what, name, t, shape, dtype, device):
-    """ff_heads of a tensor [n, heads, head_dim] of any strides but the last, which is 1."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
-        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {shape} of {dtype} on {device}")
+    """ff_heads of a tensor [n, heads, head_dim] of any strides but the last, which is 1.  device: number of the GPU."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {tuple(shape)} of {dtype} on device {device}")
     rs, hs, es = t.stride()
     if es != 1 and shape[2] > 1 and t.numel():
         _refuse(what, f"{name}: the elements of a head have to lie side by side")
@@ -481,52 +481,49 @@ def _array(what, name, t, length, dtype, device):
     """Address of a contiguous tensor of at least `length` elements; None stays None."""
     if t is None:
         return None
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or t.device != device or t.numel() < length or not t.is_contiguous():
-        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {length} contiguous elements of {dtype} on {device}")
+    if t.dtype is not dtype or t.get_device() != device or t.numel() < length or not t.is_contiguous():
+        _refuse(what, f"{name}: {tuple(t.shape)} of {t.dtype} on {t.device}, wanted {length} contiguous elements of {dtype} on device {device}")
     return t.data_ptr()
 
 
-class _On:
-    """Makes a tensor's device the current one for a call, where it is not."""
+# The number of the current device, 0.1 us; torch.cuda's function takes 0.25
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
-    def __init__(self, what, t):
-        if not t.is_cuda:
-            _refuse(what, "the tensors have to be on a GPU")
-        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return _stream()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _off_device(what, device):
+    """Is a tensor's device another one than the current?"""
+    if device < 0:
+        _refuse(what, "the tensors have to be on a GPU")
+    return device != _current_device()
 
 
 def _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm, key_offsets, key_G):
     """(ff_attention_shape, ff_heads of q, of k and of v, dtype code)"""
-    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _FF_DTYPE:
+    dt = _FF_DTYPE.get(q.dtype)
+    if dt is None or q.dim() != 3 or k.dim() != 3:
         _refuse(what, "q, k and v are [rows, heads, head_dim] of float32, bfloat16 or float16")
-    (nq, H, D), (nk, K, _), dev = q.shape, k.shape, q.device
-    hq = _heads(what, "q", q, (nq, H, D), q.dtype, dev)
-    hk = _heads(what, "k", k, (nk, K, D), q.dtype, dev)
-    hv = _heads(what, "v", v, (nk, K, D), q.dtype, dev)
+    shape, dtype, dev = q.shape, q.dtype, q.get_device()
+    kshape = k.shape
+    (nq, H, D), (nk, K, Dk) = shape, kshape
+    hq = _heads(what, "q", q, shape, dtype, dev)
+    hk = _heads(what, "k", k, kshape if Dk == D else (nk, K, D), dtype, dev)
+    hv = _heads(what, "v", v, kshape, dtype, dev)
     if group_offsets is None:
         _refuse(what, "group_offsets is missing")
     i32, mg = torch.int32, int(max_groups)
-    lq = _GroupListC(_array(what, "perm", perm, nq, i32, dev), _array(what, "group_offsets", group_offsets, mg + 1, i32, dev), nq, G)
+    lq = (_array(what, "perm", perm, nq, i32, dev), _array(what, "group_offsets", group_offsets, mg + 1, i32, dev), nq, G)
     if key_offsets is None:
         if key_perm is not None or key_G is not None or nk != nq:
             _refuse(what, "keys with a list of their own need key_offsets")
         lk = lq
     else:
-        lk = _GroupListC(_array(what, "key_perm", key_perm, nk, i32, dev),
-                         _array(what, "key_offsets", key_offsets, mg + 1, i32, dev), nk, nk if key_G is None else key_G)
-        lk.G = max(lk.G, 1) if key_G is None else lk.G
+        lk = (_array(what, "key_perm", key_perm, nk, i32, dev), _array(what, "key_offsets", key_offsets, mg + 1, i32, dev), nk,
+              max(nk, 1) if key_G is None else key_G)
+    if key_mask is not None and key_mask.dtype is torch.bool:
+        key_mask = key_mask.view(torch.uint8)
     s = _AttentionShapeC(H, K, D, D ** -0.5 if scale is None else scale, _array(what, "num_groups", num_groups, 1, i32, dev), mg,
-                         lq, lk, _array(what, "key_mask", key_mask, nk, (torch.uint8, torch.bool), dev))
-    return s, hq, hk, hv, _FF_DTYPE[q.dtype]
+                         lq, lk, _array(what, "key_mask", key_mask, nk, torch.uint8, dev))
+    return s, hq, hk, hv, dt
 
 
 def ff_attention_workspace_bytes(heads, kv_heads, head_dim, nq, max_groups, G, dtype, nk=None, key_G=None):
@@ -557,19 +554,18 @@ def ff_attention(q, k, v, perm, group_offsets, num_groups, max_groups, G, scale=
     lib = load_library()
     s, hq, hk, hv, dt = _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm,
                                          key_offsets, key_G)
-    with _On(what, q) as stream:
-        if out is None:
-            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        if lse is None and want_lse:
-            lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
-        ho = _heads(what, "out", out, tuple(q.shape), q.dtype, q.device)
-        ws = workspace
-        if ws is None:
-            need = lib.ff_attention_workspace_bytes(C.byref(s), dt)
-            ws = _workspace(need, q.device) if need else None
-        st = lib.ff_attention(C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(ho),
-                              _array(what, "lse", lse, q.shape[0] * q.shape[1], torch.float32, q.device), dt,
-                              *(_aligned(ws) if ws is not None else (None, 0)), stream)
+    shape, dev = q.shape, q.get_device()
+    if _off_device(what, dev):
+        with torch.cuda.device(dev):
+            return ff_attention(q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm, key_offsets, key_G,
+                                out, lse, want_lse, workspace)
+    if out is None:
+        out = torch.zeros(shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.zeros(shape[:2], dtype=torch.float32, device=q.device)
+    ho = _heads(what, "out", out, shape, q.dtype, dev)
+    st = lib.ff_attention(s, hq, hk, hv, ho, _array(what, "lse", lse, shape[0] * shape[1], torch.float32, dev), dt,
+                          *_room(lib.ff_attention_workspace_bytes, s, dt, workspace, q), _raw_stream(dev))
     _check(st, what)
     return out, lse
 
@@ -582,24 +578,36 @@ def ff_attention_backward(q, k, v, out, lse, dout, perm, group_offsets, num_grou
     lib = load_library()
     s, hq, hk, hv, dt = _attention_shape(what, q, k, v, perm, group_offsets, num_groups, max_groups, G, scale, key_mask, key_perm,
                                          key_offsets, key_G)
-    shape, kshape, dev = tuple(q.shape), tuple(k.shape), q.device
     if lse is None:
         _refuse(what, "lse is missing")
-    with _On(what, q) as stream:
-        new = lambda t, sh: torch.zeros(sh, dtype=q.dtype, device=dev) if t is None else t  # noqa: E731
-        dq, dk, dv = new(dq, shape), new(dk, kshape), new(dv, kshape)
-        more = [_heads(what, name, t, sh, q.dtype, dev) for name, t, sh in
-                (("out", out, shape), ("dout", dout, shape), ("dq", dq, shape), ("dk", dk, kshape), ("dv", dv, kshape))]
-        ho, hg, hdq, hdk, hdv = (C.byref(m) for m in more)
-        ws = workspace
-        if ws is None:
-            need = lib.ff_attention_backward_workspace_bytes(C.byref(s), dt)
-            ws = _workspace(need, dev) if need else None
-        st = lib.ff_attention_backward(C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), ho,
-                                       _array(what, "lse", lse, shape[0] * shape[1], torch.float32, dev), hg, hdq, hdk, hdv, dt,
-                                       *(_aligned(ws) if ws is not None else (None, 0)), stream)
+    shape, kshape, dtype, dev = q.shape, k.shape, q.dtype, q.get_device()
+    if _off_device(what, dev):
+        with torch.cuda.device(dev):
+            return ff_attention_backward(q, k, v, out, lse, dout, perm, group_offsets, num_groups, max_groups, G, scale, key_mask,
+                                         key_perm, key_offsets, key_G, dq, dk, dv, workspace)
+    if dq is None:
+        dq = torch.zeros(shape, dtype=dtype, device=q.device)
+    if dk is None:
+        dk = torch.zeros(kshape, dtype=dtype, device=q.device)
+    if dv is None:
+        dv = torch.zeros(kshape, dtype=dtype, device=q.device)
+    st = lib.ff_attention_backward(
+        s, hq, hk, hv, _heads(what, "out", out, shape, dtype, dev), _array(what, "lse", lse, shape[0] * shape[1], torch.float32, dev),
+        _heads(what, "dout", dout, shape, dtype, dev), _heads(what, "dq", dq, shape, dtype, dev), _heads(what, "dk", dk, kshape, dtype, dev),
+        _heads(what, "dv", dv, kshape, dtype, dev), dt, *_room(lib.ff_attention_backward_workspace_bytes, s, dt, workspace, q),
+        _raw_stream(dev))
     _check(st, what)
     return dq, dk, dv
+
+
+def _room(query, s, dt, workspace, q):
+    """Address and size of the workspace: the caller's, or as large a one as the call needs."""
+    if workspace is None:
+        need = query(s, dt)
+        if not need:
+            return None, 0
+        workspace = _workspace(need, q.device)
+    return _aligned(workspace)
 
 
 def ff_rotary_frequencies(pairs, axes=1, base=10000.0, factor=1.0, original_length=0.0, low_turns=1.0, high_turns=32.0,
@@ -616,23 +624,32 @@ def ff_rotary(q, k, positions, freqs, layout=FF_ROTARY_HALF, amplitude=1.0, inve
     coords[:, 1:], with freqs float64 [axes, pairs].  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
     what = "ff_rotary"
     lib = load_library()
-    if q.dim() != 3 or q.dtype not in _FF_DTYPE or (k is not None and k.dim() != 3) or freqs.dim() != 2:
+    dt = _FF_DTYPE.get(q.dtype)
+    if dt is None or q.dim() != 3 or (k is not None and k.dim() != 3) or freqs.dim() != 2:
         _refuse(what, "q and k are [rows, heads, head_dim] of float32, bfloat16 or float16, freqs is [axes, pairs]")
-    (n, H, D), dev, (axes, pairs) = q.shape, q.device, freqs.shape
-    if positions.dtype != torch.int32 or positions.device != dev or tuple(positions.shape) not in ([(n,), (n, 1)] if axes == 1 else [(n, axes)]):
-        _refuse(what, f"positions: {tuple(positions.shape)} of {positions.dtype} on {positions.device}, wanted int32 {(n, axes)} on {dev}")
-    spec = _RotarySpecC(axes, pairs, layout, int(bool(inverse)), amplitude, _array(what, "freqs", freqs, axes * pairs, torch.float64, dev))
-    stride = positions.stride() + (1,)
-    with _On(what, q) as stream:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev) if q_out is None else q_out
-        hq, hqo = _heads(what, "q", q, (n, H, D), q.dtype, dev), _heads(what, "q_out", q_out, (n, H, D), q.dtype, dev)
-        hk = hko = None
-        K = 0
-        if k is not None:
-            K = k.shape[1]
-            k_out = torch.empty(k.shape, dtype=q.dtype, device=dev) if k_out is None else k_out
-            hk, hko = _heads(what, "k", k, (n, K, D), q.dtype, dev), _heads(what, "k_out", k_out, (n, K, D), q.dtype, dev)
-        st = lib.ff_rotary(hq, hqo, H, hk, hko, K, n, D, _ptr(positions), stride[0], stride[1], C.byref(spec),
-                           _FF_DTYPE[q.dtype], stream)
+    shape, dtype, dev, (axes, pairs) = q.shape, q.dtype, q.get_device(), freqs.shape
+    n, H, D = shape
+    placed = positions.shape
+    if positions.dtype is not torch.int32 or positions.get_device() != dev or not (placed == (n, axes) or (axes == 1 and placed == (n,))):
+        _refuse(what, f"positions: {tuple(placed)} of {positions.dtype} on {positions.device}, wanted int32 {(n, axes)} on device {dev}")
+    spec = _RotarySpecC(axes, pairs, layout, 1 if inverse else 0, amplitude, _array(what, "freqs", freqs, axes * pairs, torch.float64, dev))
+    hq = _heads(what, "q", q, shape, dtype, dev)
+    if _off_device(what, dev):
+        with torch.cuda.device(dev):
+            return ff_rotary(q, k, positions, freqs, layout, amplitude, inverse, q_out, k_out)
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=dtype, device=q.device)
+    hqo = _heads(what, "q_out", q_out, shape, dtype, dev)
+    hk, hko, K = None, None, 0
+    if k is not None:
+        kshape = k.shape
+        K = kshape[1]
+        hk = _heads(what, "k", k, kshape if kshape[0] == n and kshape[2] == D else (n, K, D), dtype, dev)
+        if k_out is None:
+            k_out = torch.empty(kshape, dtype=dtype, device=q.device)
+        hko = _heads(what, "k_out", k_out, kshape, dtype, dev)
+    stride = positions.stride()
+    st = lib.ff_rotary(hq, hqo, H, hk, hko, K, n, D, positions.data_ptr(), stride[0], stride[-1] if len(stride) > 1 else 1, spec, dt,
+                       _raw_stream(dev))
     _check(st, what)
     return q_out, k_out
