@@ -277,8 +277,8 @@ int ff_group_attention_path(const ff_layer_weights* w, int G, int dtype, uint32_
  * Results do not depend on timing: the same call gives the same bits.  16-bit types: products of that type with float32 sums;
  * scores, softmax, lse, delta and all sums are float32, and p and e are rounded to the type where they enter a product.
  * FF_F32: float32 throughout.
- * Limits (FF_ERR_UNSUPPORTED otherwise): head_dim 1..128, heads a multiple of kv_heads, rows < 2^31, row strides below 4 GiB, and at
- * most 2^31 - 1 workgroups a launch (tiles of 16 rows and more, times heads). */
+ * Limits (FF_ERR_UNSUPPORTED otherwise): head_dim 1..128, heads a multiple of kv_heads, rows < 2^31, strides below 4 GiB, and at most
+ * 2^31 - 1 workgroups a launch (tiles of 16 rows and more, times heads). */
 typedef struct {
   void* data; /* read only where it is an input */
   int64_t row_stride, head_stride;

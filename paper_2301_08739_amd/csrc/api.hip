@@ -98,7 +98,7 @@ bool meets_written(const HeadsIn* arrays, int count, size_t size, const void* p,
   return false;
 }
 HeadsAt heads_at(const ff_heads* x) { return {x->data, x->row_stride, x->head_stride}; }
-Heads heads_of(const ff_heads* x, size_t size) { return {(char*)x->data, x->head_stride * (int64_t)size, (uint32_t)(x->row_stride * size)}; }
+Heads heads_of(const ff_heads* x, size_t size) { return {(char*)x->data, (uint32_t)(x->row_stride * size), (uint32_t)(x->head_stride * size)}; }
 
 int check_list(const ff_group_list& l) {
   if (l.n < 0 || l.G < 1) return FF_ERR_ARG;
@@ -125,7 +125,7 @@ int check_attention_call(const ff_attention_shape* a, const HeadsIn* arrays, int
   const size_t size = elem_size(dtype), lse_bytes = (size_t)a->queries.n * a->heads * 4;
   if (const int st = check_arrays(arrays, count, size); st != FF_OK) return st;
   for (int i = 0; i < count; ++i)
-    if (arrays[i].x->row_stride > (int64_t)(UINT32_MAX / size)) return FF_ERR_UNSUPPORTED;
+    if (arrays[i].x->row_stride > (int64_t)(UINT32_MAX / size) || arrays[i].x->head_stride > (int64_t)(UINT32_MAX / size)) return FF_ERR_UNSUPPORTED;
   if ((a->max_groups > 0 && (!a->queries.offsets || !a->keys.offsets)) || (uintptr_t)lse % 4) return FF_ERR_ARG;
   const struct { const void* p; size_t bytes; bool written; } pieces[] = {
       {lse, lse_bytes, lse_written}, {workspace, need, true},

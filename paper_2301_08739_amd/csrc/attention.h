@@ -6,26 +6,22 @@ namespace ff {
 
 struct Heads {  // head h of row r begins r * rs + h * hs bytes on
   char* p;
-  int64_t hs;
-  uint32_t rs;  // (so that an address is one multiplication and addition: rows of 4 GiB and more are refused)
+  uint32_t rs, hs;  // (so that an address is two multiplications and additions: strides of 4 GiB and more are refused)
 };
 struct GroupList {
   const int32_t* perm;  // or nullptr: position p is row p
   const int32_t* off;
   int32_t n, G;
 };
-struct Div {  // quotients of numbers below 2^31 by a constant: a multiplication instead of a division a piece
+struct Div {  // quotients of numbers below 2^31 by a constant: a multiplication instead of a division
   uint32_t by, mul, shift;
 };
 inline Div make_div(uint32_t by) {
   uint32_t s = 0;
   while ((1u << s) < by) ++s;
-  const uint64_t m = (((uint64_t)1 << (32 + s)) + by - 1) / by;  // < 2^33: the top bit is added back by hand
-  return {by, (uint32_t)(m - ((uint64_t)1 << 32)), s};
+  return {by, (uint32_t)((((uint64_t)1 << (32 + s)) + by - 1) / by), s};  // less the bit of 2^32, which the addition puts back
 }
-__device__ __forceinline__ uint32_t quotient(uint32_t x, const Div& d) {
-  return d.by == 1 ? x : (uint32_t)(((uint64_t)__umulhi(x, d.mul) + x) >> d.shift);
-}
+__device__ __forceinline__ uint32_t quotient(uint32_t x, const Div& d) { return (__umulhi(x, d.mul) + x) >> d.shift; }
 
 struct Attn {
   Heads q, k, v, out, dout, dq, dk, dv;
@@ -79,7 +75,7 @@ __device__ __forceinline__ int32_t row_at(const GroupList& l, int32_t p) {
   return (uint32_t)r < (uint32_t)l.n ? r : -1;
 }
 template <typename T> __device__ __forceinline__ T* row_of_head(const Heads& x, int32_t row, int32_t h) {
-  return reinterpret_cast<T*>(x.p + h * x.hs + (uint64_t)(uint32_t)row * x.rs);
+  return reinterpret_cast<T*>(x.p + (uint64_t)(uint32_t)h * x.hs + (uint64_t)(uint32_t)row * x.rs);
 }
 
 }  // namespace ff

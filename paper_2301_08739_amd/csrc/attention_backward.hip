@@ -64,6 +64,7 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
   const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   T *const et = keys_all[wave], *const qs = rows_all[wave][0], *const gs = rows_all[wave][1];
   float *const offs = stats_all[wave][0], *const deltas = stats_all[wave][1];
+  touch_arguments(a);
   const uint32_t item = blockIdx.x * 4 + wave;
   if (item >= items.total) return;
   const uint32_t group = quotient(item, items.heads);
@@ -80,9 +81,9 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
   if (a.mask) {
     uint8_t seen[RK / 16];
 #pragma unroll
-    for (int t = 0; t < RK / 16; ++t) seen[t] = key[t] < 0 ? 0 : a.mask[key[t]];
+    for (int t = 0; t < RK / 16; ++t) seen[t] = a.mask[key[t] < 0 ? 0 : key[t]];
 #pragma unroll
-    for (int t = 0; t < RK / 16; ++t) live |= seen[t] ? 1u << t : 0u;
+    for (int t = 0; t < RK / 16; ++t) live |= key[t] >= 0 && seen[t] ? 1u << t : 0u;
   } else {
 #pragma unroll
     for (int t = 0; t < RK / 16; ++t) live |= key[t] >= 0 ? 1u << t : 0u;
@@ -111,11 +112,12 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
     }
   };
   if (rows > 0) fetch(0);
+  if (PER % 4 == 0 || g4 < PER) {
 #pragma unroll
-  for (int t = 0; t < RK / 16; ++t)
+    for (int t = 0; t < RK / 16; ++t)
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
-      if (f * 4 + g4 < PER) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LD + f * KF + g4 * E) = t < KT ? kf[t < KT ? t : 0][f].q : u32x4{0u, 0u, 0u, 0u};
+      for (int f = 0; f < NF; ++f) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LD + f * KF + g4 * E) = t < KT ? kf[t < KT ? t : 0][f].q : u32x4{0u, 0u, 0u, 0u};
+  }
   wave_sync();
   Piece kc[DT][KP];
 #pragma unroll
@@ -148,7 +150,10 @@ __global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1
       qr[f] = qf[f];
       gr[f] = gf[f];
       delta += dot_pieces<T>(gf[f], of[f]);
-      if (f * 4 + g4 < PER) {
+    }
+    if (PER % 4 == 0 || g4 < PER) {
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
         *reinterpret_cast<u32x4*>(qs + i * LD + f * KF + g4 * E) = qf[f].q;
         *reinterpret_cast<u32x4*>(gs + i * LD + f * KF + g4 * E) = gf[f].q;
       }
@@ -251,6 +256,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
   __shared__ __attribute__((aligned(16))) T gs[NB][BQ * LD];
   __shared__ __attribute__((aligned(16))) float offs[NB][BQ], deltas[NB][BQ];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
+  touch_arguments(a);
   const uint32_t work = in_order(order);
   if (work >= order.total) return;
   const uint32_t row_of_work = work / tg.tiles;
@@ -430,6 +436,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LD];
   __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
+  touch_arguments(a);
   const uint32_t work = in_order(order);
   if (work >= order.total) return;
   const uint32_t row_of_work = work / tg.tiles;

@@ -17,6 +17,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
   const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   T* const vs = vs_all[wave];
   float* const bias = bias_all[wave];
+  touch_arguments(a);
   const uint32_t item = blockIdx.x * 4 + wave;
   if (item >= items.total) return;
   const uint32_t rest = quotient(item, items.heads), group = quotient(rest, items.parts);
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
   if (a.mask) {
     uint8_t seen[RK / 16];
 #pragma unroll
-    for (int t = 0; t < RK / 16; ++t) seen[t] = key[t] < 0 ? 0 : a.mask[key[t]];
+    for (int t = 0; t < RK / 16; ++t) seen[t] = a.mask[key[t] < 0 ? 0 : key[t]];
 #pragma unroll
     for (int t = 0; t < RK / 16; ++t)
       if (!seen[t]) key[t] = -1;
@@ -58,12 +59,15 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
 #pragma unroll
       for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
   }
+  if (g4 == 0) {
 #pragma unroll
-  for (int t = 0; t < RK / 16; ++t) {
+    for (int t = 0; t < RK / 16; ++t) bias[t * 16 + i] = key[t] >= 0 ? 0.f : -INFINITY;
+  }
+  if (PER % 4 == 0 || g4 < PER) {
 #pragma unroll
-    for (int c = 0; c < (PER + 3) / 4; ++c)
-      if (c * 4 + g4 < PER) *reinterpret_cast<u32x4*>(vs + (t * 16 + i) * LD + (c * 4 + g4) * E) = vr[t][c].q;
-    if (g4 == 0) bias[t * 16 + i] = key[t] >= 0 ? 0.f : -INFINITY;
+    for (int t = 0; t < RK / 16; ++t)
+#pragma unroll
+      for (int c = 0; c < (PER + 3) / 4; ++c) *reinterpret_cast<u32x4*>(vs + (t * 16 + i) * LD + (c * 4 + g4) * E) = vr[t][c].q;
   }
   wave_sync();
   Piece vf[DT][KP];
@@ -111,7 +115,7 @@ __global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group
       for (int d = 0; d < DT; ++d) o[d] = mma<T>(vf[d][t], p, o[d]);
     }
     if (q.row >= 0) {
-      const float by = sum == 0.f ? 0.f : 1.f / sum;  // no key: zero
+      const float by = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);  // no key: zero
       T* out = row_of_head<T>(a.out, q.row, q.h);
 #pragma unroll
       for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
@@ -142,6 +146,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   __shared__ __attribute__((aligned(16))) T vs[NB][BK * LDV];
   __shared__ __attribute__((aligned(16))) float bias[NB][BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g4 = lane >> 4, i = lane & 15;
+  touch_arguments(a);
   const uint32_t work = in_order(order);
   if (work >= order.total) return;
   const uint32_t row_of_work = work / tg.tiles;
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       }
       continue;
     }
-    const float by = total == 0.f ? 0.f : 1.f / total;  // no key: zero
+    const float by = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);  // no key: zero
     T* out = row_of_head<T>(a.out, q[u].row, q[u].h);
 #pragma unroll
     for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[u][d] * by, a.D);

@@ -193,6 +193,12 @@ __device__ __forceinline__ float over_lanes16_sum(float v) {
 // scale is negative; a scale of zero as next to nothing.
 __device__ __forceinline__ float exponent_factor(const Attn& a) { return a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e; }
 
+// A launch's arguments lie in a few lines of memory that no cache holds yet; asked for one by one, as they are first used, each is a
+// trip.  So one word of every line is asked for at the start, all together.
+__device__ __forceinline__ void touch_arguments(const Attn& a) {
+  asm volatile("" ::"s"(a.q.p), "s"(a.v.p), "s"(a.dout.p), "s"(a.dk.p), "s"(a.lse), "s"(a.num_groups), "s"(a.kl.perm), "s"(a.mask));
+}
+
 // ---- which tile of which group ---------------------------------------------------------------------------
 // Tiles of B rows (positions times `share` heads that have their keys in common).  Groups of about the same length: tile t is tile
 // t % per_group of group t / per_group.  Else, so that long lists of mostly short groups launch few empty workgroups: group g owns
