@@ -52,178 +52,202 @@ template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a
 // ---- short groups: a wavefront holds all keys, values and their gradients of a group and key head ---------------
 // Scores with the queries down and the keys across (Q K^T): a lane holds scores of one key, and p and e are the right operands of
 // (dv)^T = dout^T p and (dk)^T = q^T e as they lie in the registers.  For (dq)^T = K^T e^T e goes through LDS once, which turns it.
-// Queries by 16, delta from their own rows on the way.
-template <typename T, int DP, int KT, bool WHOLE>
-__global__ __launch_bounds__(256, KT * DP <= (sizeof(T) == 4 ? 96 : 160) ? 2 : 1) void k_attention_backward_group(Attn a, Items items) {
-  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16;
+// All rows come and go through LDS, for the workgroup's heads together.  Region A: keys, then e, then dk; B: values, then queries (and dq
+// in their places) and dout by CH rows, then dv.  delta is summed where the rows of dout and out come in.
+template <typename T, int DP, int KT, int HW, bool WHOLE>
+__global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 128 : 96) : 192) ? 2 : 1) void k_attention_backward_group(Attn a, Items items) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * HW;
+  constexpr int CH = DP * (int)sizeof(T) <= 32 ? 32 : 16;  // (one piece of each array a thread, two of rows of 128 bytes)
   constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 16 + PAD;
-  constexpr int PER = DP * (int)sizeof(T) / 16;
-  __shared__ __attribute__((aligned(16))) T keys_all[4][RK * (LD > LDE ? LD : LDE)];  // keys, then e
-  __shared__ __attribute__((aligned(16))) T rows_all[4][2][16 * LD];                  // q and dout
-  __shared__ __attribute__((aligned(16))) float stats_all[4][2][16];
-  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  T *const et = keys_all[wave], *const qs = rows_all[wave][0], *const gs = rows_all[wave][1];
-  float *const offs = stats_all[wave][0], *const deltas = stats_all[wave][1];
+  constexpr int PITCH_A = RK * (LD > LDE ? LD : LDE);
+  constexpr bool ONE = HW * (PITCH_A + KT * 16 * LD) * sizeof(T) > 78 * 1024;  // two workgroups would not fit: values and dv by A too
+  constexpr int PITCH_B = (!ONE && KT * 16 > 2 * CH ? KT * 16 : 2 * CH) * LD;
+  typedef KeyPieces<T, DP, HW, KT * 16> KeyP;
+  typedef QueryPieces<T, DP, HW, CH> QueryP;
+  constexpr int PER = QueryP::H::PER, UQ = QueryP::H::U;
+  __shared__ __attribute__((aligned(16))) T region_a[HW * PITCH_A], region_b[HW * PITCH_B];
+  __shared__ __attribute__((aligned(16))) float bias[KT * 16], offs_all[HW][CH], deltas_all[HW][CH];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   touch_arguments(a);
-  const uint32_t item = blockIdx.x * 4 + wave;
-  if (item >= items.total) return;
-  const uint32_t group = quotient(item, items.heads);
-  const int kh = item - group * items.heads.by;
+  const uint32_t group = quotient(blockIdx.x, items.sets);
+  const int kh0 = (blockIdx.x - group * items.sets.by) * HW, h0 = kh0 * (int)a.share.by;
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
-  const int32_t rows = sq.len * (int32_t)a.share.by;
   if ((int32_t)group >= groups_of(a)) return;
+  const int32_t PC = quotient(CH, a.share), last = sq.len;
 
-  int32_t key[RK / 16];
-  uint32_t live = 0;  // bit t: key t of this lane is one that queries look at
-  QueryTiles qt;
-  if (rows > 0) qt.ask(a, sq, i);
-  key_rows(key, a, sk, i);
-  if (a.mask) {
-    uint8_t seen[RK / 16];
+  KeyP kp;
+  QueryP qp;
+  Piece kr[KeyP::H::U], vr[KeyP::H::U], qr[UQ], gr[UQ], yr[UQ];
+  float lse[UQ];
+  kp.place(tid);
+  kp.ask(a, sk);
+  qp.place(a, tid);
+  int32_t end = PC < last ? PC : last;
+  auto fetch = [&](int32_t p0) {
+    qp.look(a, sq, p0, end);
+    qp.template fetch<WHOLE>(qr, a.q, h0, a.D);
+    qp.template fetch<WHOLE>(gr, a.dout, h0, a.D);
+    qp.template fetch<WHOLE>(yr, a.out, h0, a.D);
 #pragma unroll
-    for (int t = 0; t < RK / 16; ++t) seen[t] = a.mask[key[t] < 0 ? 0 : key[t]];
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t) live |= key[t] >= 0 && seen[t] ? 1u << t : 0u;
-  } else {
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t) live |= key[t] >= 0 ? 1u << t : 0u;
-  }
-  Piece kf[KT][NF], vf[KT][NF];
-#pragma unroll
-  for (int t = 0; t < KT; ++t)
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      kf[t][f] = load_piece<T, WHOLE>(a.k, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
-      vf[t][f] = load_piece<T, WHOLE>(a.v, live >> t & 1 ? key[t] : -1, kh, f * KF + g4 * E, a.D);
-    }
-  // The rows of the next sixteen queries are on their way while these are worked on, and their numbers before them
-  QueryRow q;
-  Piece qf[NF], gf[NF], of[NF];
-  float lse;
-  auto fetch = [&](int32_t r0) {
-    q = qt.row(a, sq, kh, r0 + i);
-    qt.ask(a, sq, r0 + 16 + i);
-    lse = q.row >= 0 ? a.lse[stat_at(a, q.row, q.h)] : -INFINITY;
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
-      gf[f] = load_piece<T, WHOLE>(a.dout, q.row, q.h, f * KF + g4 * E, a.D);
-      of[f] = load_piece<T, WHOLE>(a.out, q.row, q.h, f * KF + g4 * E, a.D);
-    }
+    for (int u = 0; u < UQ; ++u) lse[u] = qp.row[u] >= 0 ? a.lse[stat_at(a, qp.row[u], h0 + qp.h[u])] : -INFINITY;
+    if (p0 + PC < last) qp.ask(a, sq, p0 + PC);
   };
-  if (rows > 0) fetch(0);
-  if (PER % 4 == 0 || g4 < PER) {
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t)
-#pragma unroll
-      for (int f = 0; f < NF; ++f) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LD + f * KF + g4 * E) = t < KT ? kf[t < KT ? t : 0][f].q : u32x4{0u, 0u, 0u, 0u};
+  if (last > 0) qp.ask(a, sq, 0);
+  kp.look(a, sk);
+  kp.template fetch<WHOLE>(kr, a.k, kh0, a.D);
+  kp.template fetch<WHOLE>(vr, a.v, kh0, a.D);
+  if (last > 0) fetch(0);
+  T *const ta = region_a + wave * PITCH_A, *const qs = region_b + wave * PITCH_B, *const gs = qs + CH * LD;
+  float *const offs = offs_all[wave], *const deltas = deltas_all[wave];
+  if constexpr (KT * 16 < RK) {  // keys that make the last piece whole
+    for (int x = lane; x < (RK - KT * 16) * LD / E; x += 64) *reinterpret_cast<u32x4*>(ta + KT * 16 * LD + x * E) = u32x4{0u, 0u, 0u, 0u};
   }
-  wave_sync();
-  Piece kc[DT][KP];
+  kp.put(region_a, PITCH_A, LD, kr);
+  if (!ONE) kp.put(region_b, PITCH_B, LD, vr);
+  if (kp.head == 0 && kp.c == 0) {
+#pragma unroll
+    for (int u = 0; u < KeyP::H::U; ++u)
+      if (kp.first + u * KeyP::H::STEP < KT * 16) bias[kp.first + u * KeyP::H::STEP] = kp.live >> u & 1 ? 0.f : -INFINITY;
+  }
+  __syncthreads();
+  auto rows_of = [&](const T* tile, int r, int f) {
+    Piece p;
+    if constexpr (DP < KF) {  // zero behind the row's end
+      p = row_piece(tile, LD, r, g4 * E % DP);
+      if (g4 * E >= DP) p.q = u32x4{0u, 0u, 0u, 0u};
+    } else {
+      p = row_piece(tile, LD, r, f * KF + g4 * E);
+    }
+    return p;
+  };
+  Piece kf[KT][NF], vf[KT][NF], kc[DT][KP];
+  uint32_t live = 0;  // bit t: key t of this lane is one that queries look at
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    if (bias[t * 16 + i] == 0.f) live |= 1u << t;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      kf[t][f] = rows_of(ta, t * 16 + i, f);
+      if (!ONE) vf[t][f] = rows_of(qs, t * 16 + i, f);
+      if (a.scale < 0.f) kf[t][f] = negated<T>(kf[t][f]);
+    }
+  }
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int t = 0; t < KP; ++t) kc[d][t] = column_piece(et, LD, t * 16 * TILES, d * 16, lane);
-  wave_sync();
-  if constexpr (KT * 16 < RK) {  // e of the keys that make the last piece whole
-    for (int x = lane; x < (RK - KT * 16) * LDE / E; x += 64) *reinterpret_cast<u32x4*>(et + KT * 16 * LDE + x * E) = u32x4{0u, 0u, 0u, 0u};
-  }
-
-  const float c = exponent_factor(a);
-  if (a.scale < 0.f) {
+    for (int t = 0; t < KP; ++t) kc[d][t] = column_piece(ta, LD, t * 16 * TILES, d * 16, lane);
+  if constexpr (ONE) {
+    __syncthreads();
+    kp.put(region_a, PITCH_A, LD, vr);
+    __syncthreads();
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
+      for (int f = 0; f < NF; ++f) vf[t][f] = rows_of(ta, t * 16 + i, f);
   }
+  wave_sync();
+  if constexpr (KT * 16 < RK) {  // and e of them
+    for (int x = lane; x < (RK - KT * 16) * LDE / E; x += 64) *reinterpret_cast<u32x4*>(ta + KT * 16 * LDE + x * E) = u32x4{0u, 0u, 0u, 0u};
+  }
+  const float c = exponent_factor(a);
   f32x4 dk[KT][DT], dv[KT][DT];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = all4(0.f);
 
-  for (int32_t r0 = 0; r0 < rows; r0 += 16) {
-    float delta = 0.f;
-    Piece qr[NF], gr[NF];
+  for (int32_t p0 = 0; p0 < last; p0 += PC) {
+    __syncthreads();  // values, or the last chunk's rows, have been read
+    qp.put(region_b, PITCH_B, LD, qr);
+    qp.put(region_b + CH * LD, PITCH_B, LD, gr);
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      qr[f] = qf[f];
-      gr[f] = gf[f];
-      delta += dot_pieces<T>(gf[f], of[f]);
+    for (int u = 0; u < UQ; ++u) {
+      float delta = dot_pieces<T>(gr[u], yr[u]);
+#pragma unroll
+      for (int d = 1; d < PER; d *= 2) delta += __shfl_xor(delta, d);
+      if (qp.c == 0 && qp.v[u] < CH) {
+        offs_all[qp.w[u]][qp.v[u]] = score_start(lse[u], c);
+        deltas_all[qp.w[u]][qp.v[u]] = delta * -kLower<T>;
+      }
     }
-    if (PER % 4 == 0 || g4 < PER) {
+    const QueryP now = qp;
+    const int32_t rows = (end - p0) * (int32_t)a.share.by;
+    if (p0 + PC < last) {
+      end = p0 + 2 * PC < last ? p0 + 2 * PC : last;
+      fetch(p0 + PC);
+    }
+    __syncthreads();
+    for (int32_t r0 = 0; r0 < rows; r0 += 16) {
+      const f32x4 fo = *reinterpret_cast<const f32x4*>(offs + r0 + g4 * 4), fd = *reinterpret_cast<const f32x4*>(deltas + r0 + g4 * 4);
+      Piece qf[NF], gf[NF], qc[DT], gc[DT];
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
-        *reinterpret_cast<u32x4*>(qs + i * LD + f * KF + g4 * E) = qf[f].q;
-        *reinterpret_cast<u32x4*>(gs + i * LD + f * KF + g4 * E) = gf[f].q;
+        qf[f] = rows_of(qs, r0 + i, f);
+        gf[f] = rows_of(gs, r0 + i, f);
       }
-    }
-    delta = over_lanes16_sum(delta) * -kLower<T>;
-    if (g4 == 0) {
-      offs[i] = score_start(lse, c);
-      deltas[i] = delta;
-    }
-    const QueryRow now = q;
-    if (r0 + 16 < rows) fetch(r0 + 16);
-    wave_sync();
-    const f32x4 fo = *reinterpret_cast<const f32x4*>(offs + g4 * 4), fd = *reinterpret_cast<const f32x4*>(deltas + g4 * 4);
-    Piece qc[DT], gc[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      qc[d] = column_half(qs, LD, 0, d * 16, lane);
-      gc[d] = column_half(gs, LD, 0, d * 16, lane);
-    }
-#pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      f32x4 s = fo, dp = dp_start<T>(fd);
-#pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        s = mma<T>(qr[f], kf[t][f], s);
-        dp = mma<T>(gr[f], vf[t][f], dp);
-      }
-      p_and_e<T>(s, dp, c, fd);
-      const bool here = live >> t & 1;
-      if (!__all(here)) {  // keys that no query looks at
-#pragma unroll
-        for (int r = 0; r < 4; ++r) dp[r] = here ? dp[r] : 0.f;
-      }
-      const Piece p = as_half<T>(s), e = as_half<T>(dp);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        dv[t][d] = mma_half<T>(gc[d], p, dv[t][d]);
-        dk[t][d] = mma_half<T>(qc[d], e, dk[t][d]);
+        qc[d] = column_half(qs, LD, r0, d * 16, lane);
+        gc[d] = column_half(gs, LD, r0, d * 16, lane);
       }
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.q;
-      else                          *reinterpret_cast<s16x4*>(et + (t * 16 + i) * LDE + g4 * 4) = e.s[0];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        f32x4 s = fo, dp = dp_start<T>(fd);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          s = mma<T>(qf[f], kf[t][f], s);
+          dp = mma<T>(gf[f], vf[t][f], dp);
+        }
+        p_and_e<T>(s, dp, c, fd);
+        const bool here = live >> t & 1;
+        if (!__all(here)) {  // keys that no query looks at
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dp[r] = here ? dp[r] : 0.f;
+        }
+        const Piece p = as_half<T>(s), e = as_half<T>(dp);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          dv[t][d] = mma_half<T>(gc[d], p, dv[t][d]);
+          dk[t][d] = mma_half<T>(qc[d], e, dk[t][d]);
+        }
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4*>(ta + (t * 16 + i) * LDE + g4 * 4) = e.q;
+        else                          *reinterpret_cast<s16x4*>(ta + (t * 16 + i) * LDE + g4 * 4) = e.s[0];
+      }
+      wave_sync();
+      f32x4 dq[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) dq[d] = all4(0.f);
+#pragma unroll
+      for (int t = 0; t < KP; ++t) {
+        const Piece e = column_piece(ta, LDE, t * 16 * TILES, 0, lane);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dq[d] = mma<T>(kc[d][t], e, dq[d]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) store4<T, true>(qs + (r0 + i) * LD, d * 16 + g4 * 4, dq[d] * a.scale, DP);  // over their queries
+      wave_sync();
     }
-    wave_sync();
-    f32x4 dq[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) dq[d] = all4(0.f);
-#pragma unroll
-    for (int t = 0; t < KP; ++t) {
-      const Piece e = column_piece(et, LDE, t * 16 * TILES, 0, lane);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) dq[d] = mma<T>(kc[d][t], e, dq[d]);
-    }
-    if (now.row >= 0) {
-      T* to = row_of_head<T>(a.dq, now.row, now.h);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) store4<T, WHOLE>(to, d * 16 + g4 * 4, dq[d] * a.scale, a.D);
-    }
-    wave_sync();
+    __syncthreads();
+    now.template store<WHOLE>(a.dq, h0, a.D, region_b, PITCH_B, LD);
   }
+  __syncthreads();
+  auto lay = [&](T* tile, const f32x4 (&x)[KT][DT], float by) {
 #pragma unroll
-  for (int t = 0; t < KT; ++t) {
-    if (key[t] < 0) continue;
-    const bool here = live >> t & 1;
-    T *tk = row_of_head<T>(a.dk, key[t], kh), *tv = row_of_head<T>(a.dv, key[t], kh);
-    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      store4<T, WHOLE>(tk, d * 16 + g4 * 4, here ? dk[t][d] * a.scale : zero, a.D);
-      store4<T, WHOLE>(tv, d * 16 + g4 * 4, here ? dv[t][d] * kLower<T> : zero, a.D);
-    }
+      for (int d = 0; d < DT; ++d) store4<T, true>(tile + (t * 16 + i) * LD, d * 16 + g4 * 4, live >> t & 1 ? x[t][d] * by : all4(0.f), DP);
+  };
+  lay(ta, dk, a.scale);
+  if (!ONE) lay(qs, dv, kLower<T>);
+  __syncthreads();
+  kp.template store<WHOLE>(a.dk, kh0, a.D, region_a, PITCH_A, LD);
+  if (!ONE) {
+    kp.template store<WHOLE>(a.dv, kh0, a.D, region_b, PITCH_B, LD);
+  } else {
+    __syncthreads();
+    lay(ta, dv, kLower<T>);
+    __syncthreads();
+    kp.template store<WHOLE>(a.dv, kh0, a.D, region_a, PITCH_A, LD);
   }
 }
 
@@ -601,7 +625,7 @@ Plan plan(const Attn& a, size_t size) {
   const int64_t rows = (int64_t)a.ql.G * share;
   p.fits = rows <= INT32_MAX - 512;
   if (!p.fits) return p;
-  p.group = holds_group(DP, a.kl.G, size) && rows <= 512;
+  p.group = holds_group(DP, a.kl.G, size) && rows <= 512 && share <= 16;
   if (p.group) {
     p.fits = (int64_t)a.max_groups * a.K <= INT32_MAX;
     return p;
@@ -629,8 +653,12 @@ Plan plan(const Attn& a, size_t size) {
 }
 
 template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, hipStream_t st) {
-  const Items items = make_items(a.max_groups, a.K, 1);
-  k_attention_backward_group<T, DP, KT, WHOLE><<<(items.total + 3) / 4, 256, 0, st>>>(a, items);
+  const int hw = heads_together(a.K);
+  const Items items = make_items(a.max_groups, a.K / hw, 1);
+  if (items.total == 0) return FF_OK;
+  if (hw == 4)      k_attention_backward_group<T, DP, KT, 4, WHOLE><<<items.total, 256, 0, st>>>(a, items);
+  else if (hw == 2) k_attention_backward_group<T, DP, KT, 2, WHOLE><<<items.total, 128, 0, st>>>(a, items);
+  else              k_attention_backward_group<T, DP, KT, 1, WHOLE><<<items.total, 64, 0, st>>>(a, items);
   return launch_status();
 }
 template <typename T, int DP, bool WHOLE> int run(Attn a, const Plan& p, char* ws, hipStream_t st) {

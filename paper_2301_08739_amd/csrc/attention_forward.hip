@@ -7,123 +7,152 @@ namespace ff {
 namespace {
 
 // ---- short groups: a wavefront holds all keys and values of a group and head ----------------------------------
-// Keys and values are read once into registers (values through LDS, which turns them), the queries go by 16 at a time.
-template <typename T, int DP, int KT, bool WHOLE>
-__global__ __launch_bounds__(256, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, Items items) {
-  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16;
-  constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, LD = DP + 16 / (int)sizeof(T), PER = DP * (int)sizeof(T) / 16;
-  __shared__ __attribute__((aligned(16))) T vs_all[4][RK * LD];
-  __shared__ __attribute__((aligned(16))) float bias_all[4][RK];
-  const int lane = threadIdx.x & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  T* const vs = vs_all[wave];
-  float* const bias = bias_all[wave];
+// Keys and values come through LDS into registers once (values turned there), the queries by CH rows, of which a wavefront takes 16 at
+// a time; results go back the way the queries came.  Region A holds keys, then queries, then results; B values.  Of 32 elements and
+// more B is A: two more barriers, and twice the wavefronts a compute unit has LDS for.
+template <typename T, int DP, int KT, int HW, bool WHOLE>
+__global__ __launch_bounds__(64 * HW, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, Items items) {
+  constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * HW;
+  constexpr int CH = DP * (int)sizeof(T) <= 32 ? 64 : DP * (int)sizeof(T) <= 64 ? 32 : 16;  // (two pieces a thread)
+  constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, LD = DP + 16 / (int)sizeof(T);
+  constexpr bool TWO = DP * sizeof(T) <= 32;
+  constexpr int PITCH = (RK > CH ? RK : CH) * LD;
+  typedef KeyPieces<T, DP, HW, KT * 16> KeyP;
+  typedef QueryPieces<T, DP, HW, CH> QueryP;
+  __shared__ __attribute__((aligned(16))) T region[TWO ? 2 : 1][HW * PITCH];
+  __shared__ __attribute__((aligned(16))) float bias[RK], lses[HW][CH];
+  T *const ra = region[0], *const rb = region[TWO ? 1 : 0];
+  const int tid = threadIdx.x, lane = tid & 63, g4 = lane >> 4, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   touch_arguments(a);
-  const uint32_t item = blockIdx.x * 4 + wave;
-  if (item >= items.total) return;
-  const uint32_t rest = quotient(item, items.heads), group = quotient(rest, items.parts);
-  const int kh = item - rest * items.heads.by;
-  const int32_t step = 16 * items.parts.by, first = 16 * (rest - group * items.parts.by);
+  const uint32_t rest = quotient(blockIdx.x, items.sets), group = quotient(rest, items.parts);
+  const int kh0 = (blockIdx.x - rest * items.sets.by) * HW, h0 = kh0 * (int)a.share.by;
   const Span sq = span_of(a.ql, group), sk = span_of(a.kl, group);
-  const int32_t rows = sq.len * (int32_t)a.share.by;
-  if ((int32_t)group >= groups_of(a) || first >= rows) return;
+  const int32_t per = (sq.len + (int32_t)items.parts.by - 1) / (int32_t)items.parts.by;
+  const int32_t first = (int32_t)(rest - group * items.parts.by) * per, last = first + per < sq.len ? first + per : sq.len;
+  if ((int32_t)group >= groups_of(a) || first >= last) return;
+  const int32_t PC = quotient(CH, a.share);  // positions of a chunk
 
-  int32_t key[RK / 16];
-  QueryTiles qt;
-  qt.ask(a, sq, first + i);
-  key_rows(key, a, sk, i);
-  QueryRow q = qt.row(a, sq, kh, first + i);
-  qt.ask(a, sq, first + step + i);
-  if (a.mask) {
-    uint8_t seen[RK / 16];
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t) seen[t] = a.mask[key[t] < 0 ? 0 : key[t]];
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t)
-      if (!seen[t]) key[t] = -1;
+  KeyP kp;
+  QueryP qp;
+  Piece kr[KeyP::H::U], vr[KeyP::H::U], qr[QueryP::H::U];
+  kp.place(tid);
+  kp.ask(a, sk);
+  qp.place(a, tid);
+  qp.ask(a, sq, first);
+  kp.look(a, sk);
+  kp.template fetch<WHOLE>(kr, a.k, kh0, a.D);
+  kp.template fetch<WHOLE>(vr, a.v, kh0, a.D);
+  int32_t end = first + PC < last ? first + PC : last;
+  qp.look(a, sq, first, end);
+  qp.template fetch<WHOLE>(qr, a.q, h0, a.D);
+  qp.ask(a, sq, first + PC);
+  if constexpr (KT * 16 < RK) {  // values of the keys that make the last piece whole
+    for (int x = tid; x < HW * (RK - KT * 16) * LD / E; x += NT) {
+      const int w = x / ((RK - KT * 16) * LD / E);
+      *reinterpret_cast<u32x4*>(rb + w * PITCH + KT * 16 * LD + (x - w * ((RK - KT * 16) * LD / E)) * E) = u32x4{0u, 0u, 0u, 0u};
+    }
   }
-  Piece kf[KT][NF], vr[RK / 16][(PER + 3) / 4], qf[NF];
+  kp.put(ra, PITCH, LD, kr);
+  if (TWO) kp.put(rb, PITCH, LD, vr);
+  if (kp.head == 0 && kp.c == 0) {
+#pragma unroll
+    for (int u = 0; u < KeyP::H::U; ++u)
+      if (kp.first + u * KeyP::H::STEP < KT * 16) bias[kp.first + u * KeyP::H::STEP] = kp.live >> u & 1 ? 0.f : -INFINITY;
+  }
+  __syncthreads();
+  T *const ta = ra + wave * PITCH, *const tb = rb + wave * PITCH;
+  Piece kf[KT][NF], vf[DT][KP];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
-    for (int f = 0; f < NF; ++f) kf[t][f] = load_piece<T, WHOLE>(a.k, key[t], kh, f * KF + g4 * E, a.D);
-#pragma unroll
-  for (int f = 0; f < NF; ++f) qf[f] = load_piece<T, WHOLE>(a.q, q.row, q.h, f * KF + g4 * E, a.D);
-#pragma unroll
-  for (int t = 0; t < RK / 16; ++t)
-#pragma unroll
-    for (int c = 0; c < (PER + 3) / 4; ++c) vr[t][c] = load_piece<T, WHOLE>(a.v, key[t], kh, (c * 4 + g4) * E, a.D);
-  const float c = exponent_factor(a);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int f = 0; f < NF; ++f) kf[t][f] = negated<T>(kf[t][f]);
+    for (int f = 0; f < NF; ++f) {
+      if constexpr (DP < KF) {  // zero behind the row's end
+        kf[t][f] = row_piece(ta, LD, t * 16 + i, g4 * E % DP);
+        if (g4 * E >= DP) kf[t][f].q = u32x4{0u, 0u, 0u, 0u};
+      } else {
+        kf[t][f] = row_piece(ta, LD, t * 16 + i, f * KF + g4 * E);
+      }
+      if (a.scale < 0.f) kf[t][f] = negated<T>(kf[t][f]);
+    }
+  if (!TWO) {
+    __syncthreads();
+    kp.put(rb, PITCH, LD, vr);
+    __syncthreads();
   }
-  if (g4 == 0) {
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t) bias[t * 16 + i] = key[t] >= 0 ? 0.f : -INFINITY;
-  }
-  if (PER % 4 == 0 || g4 < PER) {
-#pragma unroll
-    for (int t = 0; t < RK / 16; ++t)
-#pragma unroll
-      for (int c = 0; c < (PER + 3) / 4; ++c) *reinterpret_cast<u32x4*>(vs + (t * 16 + i) * LD + (c * 4 + g4) * E) = vr[t][c].q;
-  }
-  wave_sync();
-  Piece vf[DT][KP];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int t = 0; t < KP; ++t) vf[d][t] = column_piece(vs, LD, t * 16 * TILES, d * 16, lane);
+    for (int t = 0; t < KP; ++t) vf[d][t] = column_piece(tb, LD, t * 16 * TILES, d * 16, lane);
+  const float c = exponent_factor(a);
 
-  for (int32_t r0 = first; r0 < rows; r0 += step) {
-    const QueryRow next = qt.row(a, sq, kh, r0 + step + i);
-    Piece qn[NF];
+  for (int32_t p0 = first; p0 < last; p0 += PC) {
+    __syncthreads();  // keys, values and the last chunk's results have been read
+    qp.put(ra, PITCH, LD, qr);
+    QueryP now = qp;
+    const int32_t rows = (end - p0) * (int32_t)a.share.by;
+    if (p0 + PC < last) {
+      end = p0 + 2 * PC < last ? p0 + 2 * PC : last;
+      qp.look(a, sq, p0 + PC, end);
+      qp.template fetch<WHOLE>(qr, a.q, h0, a.D);
+      qp.ask(a, sq, p0 + 2 * PC);
+    }
+    __syncthreads();
+    for (int32_t r0 = 0; r0 < rows; r0 += 16) {
+      Piece qf[NF];
 #pragma unroll
-    for (int f = 0; f < NF; ++f) qn[f] = load_piece<T, WHOLE>(a.q, next.row, next.h, f * KF + g4 * E, a.D);
-    qt.ask(a, sq, r0 + 2 * step + i);
-    f32x4 s[KP * TILES];
-#pragma unroll
-    for (int t = 0; t < KP * TILES; ++t) s[t] = t < KT ? *reinterpret_cast<const f32x4*>(bias + t * 16 + g4 * 4) : all4(0.f);
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int f = 0; f < NF; ++f) s[t] = mma<T>(kf[t][f], qf[f], s[t]);
-    float top = kLowest;
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
-    top = over_lanes16_max(top);
-    top = top > kLowest ? top * c : 0.f;
-    float sum = 0.f;
-#pragma unroll
-    for (int t = 0; t < KT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[t][r] = exp2_fast(fmaf(s[t][r], c, -top));
-        sum += s[t][r];
+      for (int f = 0; f < NF; ++f) {
+        if constexpr (DP < KF) {
+          qf[f] = row_piece(ta, LD, r0 + i, g4 * E % DP);
+          if (g4 * E >= DP) qf[f].q = u32x4{0u, 0u, 0u, 0u};
+        } else {
+          qf[f] = row_piece(ta, LD, r0 + i, f * KF + g4 * E);
+        }
       }
-    sum = over_lanes16_sum(sum);
-    f32x4 o[DT];
+      f32x4 s[KP * TILES];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = all4(0.f);
+      for (int t = 0; t < KP * TILES; ++t) s[t] = t < KT ? *reinterpret_cast<const f32x4*>(bias + t * 16 + g4 * 4) : all4(0.f);
 #pragma unroll
-    for (int t = 0; t < KP; ++t) {
-      const Piece p = as_piece<T>(s + t * TILES);
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = mma<T>(vf[d][t], p, o[d]);
-    }
-    if (q.row >= 0) {
+        for (int f = 0; f < NF; ++f) s[t] = mma<T>(kf[t][f], qf[f], s[t]);
+      float top = kLowest;
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][r]);
+      top = over_lanes16_max(top);
+      top = top > kLowest ? top * c : 0.f;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[t][r] = exp2_fast(fmaf(s[t][r], c, -top));
+          sum += s[t][r];
+        }
+      sum = over_lanes16_sum(sum);
+      f32x4 o[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = all4(0.f);
+#pragma unroll
+      for (int t = 0; t < KP; ++t) {
+        const Piece p = as_piece<T>(s + t * TILES);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = mma<T>(vf[d][t], p, o[d]);
+      }
       const float by = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);  // no key: zero
-      T* out = row_of_head<T>(a.out, q.row, q.h);
+      wave_sync();
 #pragma unroll
-      for (int d = 0; d < DT; ++d) store4<T, WHOLE>(out, d * 16 + g4 * 4, o[d] * by, a.D);
-      if (a.lse && g4 == 0) a.lse[stat_at(a, q.row, q.h)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+      for (int d = 0; d < DT; ++d) store4<T, true>(ta + (r0 + i) * LD, d * 16 + g4 * 4, o[d] * by, DP);  // over the queries they are of
+      if (g4 == 0) lses[wave][r0 + i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
-    q = next;
+    __syncthreads();
+    now.template store<WHOLE>(a.out, h0, a.D, ra, PITCH, LD);
+    if (a.lse && now.c == 0) {
 #pragma unroll
-    for (int f = 0; f < NF; ++f) qf[f] = qn[f];
+      for (int u = 0; u < QueryP::H::U; ++u)
+        if (now.row[u] >= 0 && now.v[u] < CH) a.lse[stat_at(a, now.row[u], h0 + now.h[u])] = lses[now.w[u]][now.v[u]];
+    }
   }
 }
 
@@ -375,7 +404,7 @@ Plan plan(const Attn& a, size_t size) {
   const int64_t rows = (int64_t)a.ql.G * share;
   p.fits = rows <= INT32_MAX - 512;
   if (!p.fits) return p;
-  p.group = a.kl.G <= 128 && DP <= (size == 4 ? 32 : 64);
+  p.group = a.kl.G <= 128 && DP <= (size == 4 ? 32 : 64) && share <= 16;
   if (p.group) {
     const int64_t waves = (int64_t)a.max_groups * a.K, tiles = ceil_div(rows, 16);
     const int64_t want = waves ? ceil_div(kChipWaves, waves) : 1;
@@ -411,8 +440,12 @@ Plan plan(const Attn& a, size_t size) {
 }
 
 template <typename T, int DP, int KT, bool WHOLE> int group_launch(const Attn& a, const Plan& p, hipStream_t st) {
-  const Items items = make_items(a.max_groups, a.K, p.parts);
-  k_attention_group<T, DP, KT, WHOLE><<<(items.total + 3) / 4, 256, 0, st>>>(a, items);
+  const int hw = heads_together(a.K);
+  const Items items = make_items(a.max_groups, a.K / hw, p.parts);
+  if (items.total == 0) return FF_OK;
+  if (hw == 4)      k_attention_group<T, DP, KT, 4, WHOLE><<<items.total, 256, 0, st>>>(a, items);
+  else if (hw == 2) k_attention_group<T, DP, KT, 2, WHOLE><<<items.total, 128, 0, st>>>(a, items);
+  else              k_attention_group<T, DP, KT, 1, WHOLE><<<items.total, 64, 0, st>>>(a, items);
   return launch_status();
 }
 template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, float* ws, hipStream_t st) {

@@ -337,46 +337,151 @@ __device__ __forceinline__ QueryRow query_row(const Attn& a, const Span& sq, int
 }
 __device__ __forceinline__ uint64_t stat_at(const Attn& a, int32_t row, int32_t h) { return (uint64_t)(uint32_t)row * (uint32_t)a.H + (uint32_t)h; }
 
-// Rows of queries on their way to a wavefront that goes through a group's, 16 a tile: a tile's numbers are asked for two tiles before
-// it, and looked at a tile before it.
-struct QueryTiles {
-  int32_t raw;  // number of this lane's row in the next tile but one
-  __device__ __forceinline__ void ask(const Attn& a, const Span& sq, int32_t v) {
-    const int32_t* const list = a.ql.perm ? a.ql.perm : &zero_number;
-    const int32_t p = quotient(v, a.share);
-    raw = list[a.ql.perm ? sq.at + (p < sq.len ? p : sq.len - 1) : 0];
-  }
-  __device__ __forceinline__ QueryRow row(const Attn& a, const Span& sq, int kh, int32_t v) const {
-    const int32_t p = quotient(v, a.share), r = a.ql.perm ? raw : sq.at + p;
-    return {p < sq.len && (uint32_t)r < (uint32_t)a.ql.n ? r : -1, (int32_t)(kh * a.share.by + v - p * a.share.by)};
-  }
+// ---- rows of several heads into LDS ----------------------------------------------------------------------
+// Short groups: HW wavefronts take a group, a key head each.  Their heads lie side by side in a row, so the workgroup reads and writes
+// whole rows of them, a 16-byte piece a thread, and LDS is where they are dealt out to the wavefronts' own tiles (and gathered from
+// them).  A wavefront by itself would touch as many lines of memory for 32 bytes of each, head after head: the address unit was busy 78 %
+// of the time with that, and 3,750 groups of 64 rows, 8 heads of 16 took 65 us.
+template <typename T, int DP, int HW, int RMAX> struct HeadRows {
+  static constexpr int PER = DP * (int)sizeof(T) / 16, NT = 64 * HW, STEP = 64 / PER;  // STEP: rows between two pieces of a thread
+  static constexpr int U = (RMAX * PER + 63) / 64;                                     // pieces of a thread
 };
-// Rows of the first N x 16 keys of a group, this lane's of each sixteen; asked for together.
-template <int N> __device__ __forceinline__ void key_rows(int32_t (&key)[N], const Attn& a, const Span& sk, int i) {
-  if (sk.len <= 0) {
+template <typename T, bool WHOLE> __device__ __forceinline__ void store_piece(const Heads& x, int32_t row, int32_t h, int e, int D, const Piece& p) {
+  T* to = row_of_head<T>(x, row, h) + e;
+  if constexpr (WHOLE) {
+    if (e < D) *reinterpret_cast<u32x4*>(to) = p.q;
+  } else {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int t = 0; t < N; ++t) key[t] = -1;
-    return;
-  }
-  const int32_t* const list = a.kl.perm ? a.kl.perm : &zero_number;
+      for (int j = 0; j < 4; ++j)
+        if (e + j < D) to[j] = p.f[j];
+    } else {
 #pragma unroll
-  for (int t = 0; t < N; ++t) {
-    const int32_t p = t * 16 + i;
-    key[t] = list[a.kl.perm ? sk.at + (p < sk.len ? p : sk.len - 1) : 0];
-  }
-#pragma unroll
-  for (int t = 0; t < N; ++t) {
-    const int32_t p = t * 16 + i;
-    if (!a.kl.perm) key[t] = sk.at + p;
-    if (p >= sk.len || (uint32_t)key[t] >= (uint32_t)a.kl.n) key[t] = -1;
+      for (int j = 0; j < 8; ++j)
+        if (e + j < D) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(p.q[j / 2] >> (16 * (j % 2)));
+    }
   }
 }
-// Which of a launch's wavefronts this is: heads side by side, then parts of a group's queries, then groups
+// The keys of a group, R rows at most: this thread's pieces are of head `head` (of HW), element c * E on, and rows first + u * STEP.
+template <typename T, int DP, int HW, int R> struct KeyPieces {
+  typedef HeadRows<T, DP, HW, R> H;
+  int head, c, first;
+  int32_t row[H::U];  // -1: none
+  uint32_t live;      // bit u: one that queries look at
+  __device__ __forceinline__ void place(int tid) {
+    c = tid % H::PER;
+    head = tid / H::PER % HW;
+    first = tid / (H::PER * HW);
+  }
+  __device__ __forceinline__ void ask(const Attn& a, const Span& sk) {
+    const int32_t* const list = a.kl.perm ? a.kl.perm : &zero_number;
+    const bool some = sk.len > 0;
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      const int32_t p = first + u * H::STEP;
+      row[u] = list[a.kl.perm && some ? sk.at + (p < sk.len ? p : sk.len - 1) : 0];
+    }
+  }
+  __device__ __forceinline__ void look(const Attn& a, const Span& sk) {
+    live = 0;
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      const int32_t p = first + u * H::STEP;
+      if (!a.kl.perm) row[u] = sk.at + p;
+      if (p >= sk.len || p >= R || (uint32_t)row[u] >= (uint32_t)a.kl.n) row[u] = -1;
+      live |= row[u] >= 0 ? 1u << u : 0u;
+    }
+    if (a.mask) {
+      uint8_t seen[H::U];
+#pragma unroll
+      for (int u = 0; u < H::U; ++u) seen[u] = a.mask[row[u] < 0 ? 0 : row[u]];
+#pragma unroll
+      for (int u = 0; u < H::U; ++u)
+        if (!seen[u]) live &= ~(1u << u);
+    }
+  }
+  template <bool WHOLE> __device__ __forceinline__ void fetch(Piece (&x)[H::U], const Heads& from, int32_t kh0, int D) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) x[u] = load_piece<T, WHOLE>(from, live >> u & 1 ? row[u] : -1, kh0 + head, c * Mx<T>::E, D);
+  }
+  // tiles: `pitch` elements from one head's to the next
+  __device__ __forceinline__ void put(T* tiles, int pitch, int ld, const Piece (&x)[H::U]) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u)
+      if (R * H::PER % 64 == 0 || first + u * H::STEP < R) *reinterpret_cast<u32x4*>(tiles + head * pitch + (first + u * H::STEP) * ld + c * Mx<T>::E) = x[u].q;
+  }
+  template <bool WHOLE> __device__ __forceinline__ void store(const Heads& to, int32_t kh0, int D, const T* tiles, int pitch, int ld) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      if (row[u] < 0) continue;
+      Piece p;
+      p.q = *reinterpret_cast<const u32x4*>(tiles + head * pitch + (first + u * H::STEP) * ld + c * Mx<T>::E);
+      store_piece<T, WHOLE>(to, row[u], kh0 + head, c * Mx<T>::E, D, p);
+    }
+  }
+};
+// Queries by CH rows of each key head (CH / share positions times the heads that share it): piece u of a thread is of row v[u] of key
+// head w[u]'s tile.
+template <typename T, int DP, int HW, int CH> struct QueryPieces {
+  typedef HeadRows<T, DP, HW, CH> H;
+  int c;
+  int32_t raw[H::U], row[H::U], h[H::U];
+  int v[H::U], w[H::U];  // v < 0: a row beyond the chunk's
+  // Chunk that begins at position p0; there: its positions
+  __device__ __forceinline__ void place(const Attn& a, int tid) {
+    c = tid % H::PER;
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      const int t = tid / H::PER + u * (H::NT / H::PER), s = quotient(t, a.share), p = s / HW;
+      w[u] = s % HW;
+      h[u] = w[u] * a.share.by + t - s * a.share.by;
+      v[u] = p * a.share.by + t - s * a.share.by;
+      raw[u] = p;
+    }
+  }
+  __device__ __forceinline__ int position(const Attn& a, int u) const { return quotient(v[u], a.share); }
+  __device__ __forceinline__ void ask(const Attn& a, const Span& sq, int32_t p0) {
+    const int32_t* const list = a.ql.perm ? a.ql.perm : &zero_number;
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      const int32_t p = p0 + position(a, u);
+      raw[u] = list[a.ql.perm ? sq.at + (p < sq.len ? p : sq.len - 1) : 0];
+    }
+  }
+  // end: one behind the last position of the chunk
+  __device__ __forceinline__ void look(const Attn& a, const Span& sq, int32_t p0, int32_t end) {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      const int32_t p = p0 + position(a, u), r = a.ql.perm ? raw[u] : sq.at + p;
+      row[u] = p < end && (uint32_t)r < (uint32_t)a.ql.n ? r : -1;
+    }
+  }
+  template <bool WHOLE> __device__ __forceinline__ void fetch(Piece (&x)[H::U], const Heads& from, int32_t h0, int D) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) x[u] = load_piece<T, WHOLE>(from, row[u], h0 + h[u], c * Mx<T>::E, D);
+  }
+  __device__ __forceinline__ void put(T* tiles, int pitch, int ld, const Piece (&x)[H::U]) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u)
+      if (v[u] < CH) *reinterpret_cast<u32x4*>(tiles + w[u] * pitch + v[u] * ld + c * Mx<T>::E) = x[u].q;
+  }
+  template <bool WHOLE> __device__ __forceinline__ void store(const Heads& to, int32_t h0, int D, const T* tiles, int pitch, int ld) const {
+#pragma unroll
+    for (int u = 0; u < H::U; ++u) {
+      if (row[u] < 0 || v[u] >= CH) continue;
+      Piece p;
+      p.q = *reinterpret_cast<const u32x4*>(tiles + w[u] * pitch + v[u] * ld + c * Mx<T>::E);
+      store_piece<T, WHOLE>(to, row[u], h0 + h[u], c * Mx<T>::E, D, p);
+    }
+  }
+};
+// Which of a launch's workgroups this is: sets of heads, then parts of a group's queries, then groups
 struct Items {
   uint32_t total;
-  Div heads, parts;
+  Div sets, parts;
 };
-inline Items make_items(int64_t groups, int heads, int parts) { return {(uint32_t)(groups * heads * parts), make_div(heads), make_div(parts)}; }
+inline Items make_items(int64_t groups, int sets, int parts) { return {(uint32_t)(groups * sets * parts), make_div(sets), make_div(parts)}; }
+inline int heads_together(int K) { return K % 4 == 0 ? 4 : K % 2 == 0 ? 2 : 1; }
 
 // May rows of this array be read and written in pieces of 16 bytes?
 inline bool whole_pieces(const Heads& x, int D, size_t size) {
