@@ -17,17 +17,12 @@ template <> constexpr float kLower<f16_t> = 1.f / 4096.f;
 // What the products of a row's scores and of its dp start from: minus the logarithm of the row's sum, in units of the scores
 // (-infinity, every p zero, where the row has no key), and minus delta.  Half precision, whose dp is scaled first: minus delta 2^-12.
 __device__ __forceinline__ float score_start(float lse, float c) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e / c; }
-// p and e, in the places of scores and dp that began so
-template <typename T> __device__ __forceinline__ void p_and_e(f32x4& s, f32x4& dp, float c, f32x4 minus_delta) {
+// p and e, in the places of scores and dp that began so; shift: what is left to add to the exponents
+template <typename T> __device__ __forceinline__ void p_and_e(f32x4& s, f32x4& dp, float c, float shift, f32x4 minus_delta) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    if constexpr (kLift<T> > 0.f) {
-      s[r] = exp2_fast(fmaf(s[r], c, kLift<T>));
-      dp[r] = s[r] * fmaf(dp[r], kLower<T>, minus_delta[r]);
-    } else {
-      s[r] = exp2_fast(s[r] * c);
-      dp[r] = s[r] * dp[r];
-    }
+    s[r] = exp2_fast(fmaf(s[r], c, shift));
+    dp[r] = s[r] * (kLift<T> > 0.f ? fmaf(dp[r], kLower<T>, minus_delta[r]) : dp[r]);
   }
 }
 template <typename T> __device__ __forceinline__ f32x4 dp_start(f32x4 minus_delta) { return kLift<T> > 0.f ? all4(0.f) : minus_delta; }
@@ -198,7 +193,7 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 1
           s = mma<T>(qf[f], kf[t][f], s);
           dp = mma<T>(gf[f], vf[t][f], dp);
         }
-        p_and_e<T>(s, dp, c, fd);
+        p_and_e<T>(s, dp, c, kLift<T>, fd);
         const bool here = live >> t & 1;
         if (!__all(here)) {  // keys that no query looks at
 #pragma unroll
@@ -403,7 +398,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
           }
         }
 #pragma unroll
-        for (int k = 0; k < KW; ++k) p_and_e<T>(s[k][u], dp[k][u], c, l);
+        for (int k = 0; k < KW; ++k) p_and_e<T>(s[k][u], dp[k][u], c, kLift<T>, l);
       }
       Piece p[KW][PQ], e[KW][PQ];
 #pragma unroll
@@ -480,12 +475,13 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   if (t0 < t1) kt.template fetch<WHOLE>(a, sk, t0, kh, tid);
   kt.next(a, sk, t0 + 1, t1, tid);
   Piece qf[QT][NF], gf[QT][NF];
-  f32x4 s0[QT], dp0[QT];
+  f32x4 dp0[QT];
+  float shift[QT];
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
     float2 st = make_float2(-INFINITY, 0.f);
     if (q[u].row >= 0) st = a.stats[stat_at(a, q[u].row, q[u].h)];
-    s0[u] = all4(st.x);
+    shift[u] = st.x * exponent_factor(a) + kLift<T>;
     dp0[u] = all4(st.y);
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
@@ -518,16 +514,16 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
       kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
-    const bool gaps = __any(bias[buf][lane % BK] < 0.f);
 #pragma unroll
     for (int k = 0; k < BK / 16 / TILES; ++k) {
       f32x4 s[QT][TILES], dp[QT][TILES];
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
         const int r = (k * TILES + x) * 16;
+        const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + r + g4 * 4);  // minus infinity for keys that are not there
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
-          s[u][x] = s0[u];
+          s[u][x] = b;
           dp[u][x] = dp_start<T>(dp0[u]);
         }
 #pragma unroll
@@ -539,15 +535,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
             dp[u][x] = mma<T>(vf, gf[u][f], dp[u][x]);
           }
         }
-        if (gaps) {
-          const f32x4 b = *reinterpret_cast<const f32x4*>(bias[buf] + r + g4 * 4);
 #pragma unroll
-          for (int u = 0; u < QT; ++u)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[u][x][j] = b[j] < 0.f ? -INFINITY : s[u][x][j];
-        }
-#pragma unroll
-        for (int u = 0; u < QT; ++u) p_and_e<T>(s[u][x], dp[u][x], c, dp0[u]);
+        for (int u = 0; u < QT; ++u) p_and_e<T>(s[u][x], dp[u][x], c, shift[u], dp0[u]);
       }
       Piece e[QT];
 #pragma unroll

@@ -162,10 +162,10 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= 256 ? 2 : 1) void k_attention_g
 // leaves sums, maximum and total in the workspace; k_attention_join brings them together.
 //
 // The vector unit is what such a kernel waits for (an exponential takes as long as four other instructions), so little else is done a
-// score.  The products of a tile start from minus the running maximum instead of zero.  That maximum may be too low by a factor of
-// 2^8 in p (no type's range minds), so that lanes need not compare notes: only where a lane finds a score beyond that, or its row has
-// met no key yet, is the maximum made good and what was summed brought down.   Keys that are not there cost something in their own tiles
-// only.  The sum of p is one of float32 additions: a product with ones would sum the rounded p, and lse would be 2^-9 off.
+// score.  Products start from minus infinity instead of zero for keys that are not there.  The running maximum may be too low by a
+// factor of 2^8 in p (no type's range minds), so that lanes need not compare notes: only where a lane finds a score beyond that, or its
+// row has met no key yet, is the maximum made good and what was summed brought down.  The sum of p is one of float32 additions: a
+// product with ones would sum the rounded p, and lse would be 2^-9 off.
 template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) || (DP == 64 && NW == 4) ? 2 : 1) void k_attention_tiles(Attn a, TileGrid tg, Order order, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
@@ -209,22 +209,22 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   }
   const float c = exponent_factor(a), far = 8.f / c;
   f32x4 o[QT][DT], sum[QT];
-  float base[QT];   // minus the running maximum of the scores
-  float limit[QT];  // what a score above it may reach: -infinity until the row has met a key
+  float most[QT], shift[QT];  // running maximum of the scores, -infinity until the row has met a key, and what it adds to the exponents
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
-    base[u] = 0.f;
-    limit[u] = -INFINITY;
+    most[u] = -INFINITY;
+    shift[u] = 0.f;
     sum[u] = all4(0.f);
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[u][d] = all4(0.f);
   }
-  auto tile = [&](bool gaps, const T* kb, const T* vb, const float* bb) {
+  auto tile = [&](const T* kb, const T* vb, const float* bb) {
     f32x4 s[QT][BK / 16];
 #pragma unroll
     for (int k = 0; k < BK / 16; ++k) {
+      const f32x4 b = *reinterpret_cast<const f32x4*>(bb + k * 16 + g4 * 4);
 #pragma unroll
-      for (int u = 0; u < QT; ++u) s[u][k] = all4(base[u]);
+      for (int u = 0; u < QT; ++u) s[u][k] = b;
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         const Piece kf = row_piece(kb, LDK, k * 16 + i, f * KF + g4 * E);
@@ -232,18 +232,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
         for (int u = 0; u < QT; ++u) s[u][k] = mma<T>(kf, qf[u][f], s[u][k]);
       }
     }
-    if (gaps) {
-#pragma unroll
-      for (int k = 0; k < BK / 16; ++k) {
-        const f32x4 b = *reinterpret_cast<const f32x4*>(bb + k * 16 + g4 * 4);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[u][k][r] = b[r] < 0.f ? -INFINITY : s[u][k][r];
-      }
-    }
     bool raise = false;
-    float top[QT], less[QT];
+    float top[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       top[u] = s[u][0][0];
@@ -251,22 +241,20 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       for (int k = 0; k < BK / 16; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top[u] = fmaxf(top[u], s[u][k][r]);
-      less[u] = 0.f;
-      raise |= top[u] > limit[u];
+      raise |= top[u] > most[u] + far;
     }
     if (__any(raise)) {
 #pragma unroll
       for (int u = 0; u < QT; ++u) {
-        const bool met = limit[u] > 0.f;
-        const float m = over_lanes16_max(top[u]);  // above the maximum so far
-        const bool up = m > (met ? 0.f : -INFINITY);
-        const float by = up ? m : 0.f, f = met ? exp2_fast(-c * by) : 0.f;
-        sum[u] *= f;
+        const float m = over_lanes16_max(top[u]);
+        if (m > most[u]) {
+          const float f = exp2_fast(c * (most[u] - m));
+          sum[u] *= f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[u][d] *= f;
-        less[u] = -c * by;
-        base[u] -= by;
-        limit[u] = up || met ? far : limit[u];
+          for (int d = 0; d < DT; ++d) o[u][d] *= f;
+          most[u] = m;
+          shift[u] = -c * m;
+        }
       }
     }
     Piece p[QT][BK / 16 / TILES];
@@ -276,7 +264,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       for (int k = 0; k < BK / 16; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          s[u][k][r] = exp2_fast(fmaf(s[u][k][r], c, less[u]));
+          s[u][k][r] = exp2_fast(fmaf(s[u][k][r], c, shift[u]));
           sum[u][r] += s[u][k][r];
         }
 #pragma unroll
@@ -301,14 +289,12 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
-    float worst = bias[buf][lane % BK];
-    if constexpr (BK == 128) worst = fminf(worst, bias[buf][lane + 64]);
-    tile(__any(worst < 0.f), ks[buf], vs[buf], bias[buf]);
+    tile(ks[buf], vs[buf], bias[buf]);
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
     const float total = over_lanes16_sum((sum[u][0] + sum[u][1]) + (sum[u][2] + sum[u][3]));
-    const float top = limit[u] > 0.f ? -c * base[u] : kLowest;
+    const float top = most[u] > -INFINITY ? -shift[u] : kLowest;
     if (q[u].row < 0) continue;
     const int64_t at_row = stat_at(a, q[u].row, q[u].h);
     if (splits > 1) {
