@@ -14,17 +14,29 @@ template <> constexpr float kLift<f16_t> = 12.f;
 template <typename T> constexpr float kLower = 1.f;
 template <> constexpr float kLower<f16_t> = 1.f / 4096.f;
 
-// What the products of a row's scores and of its dp start from: minus the logarithm of the row's sum, in units of the scores
-// (-infinity, every p zero, where the row has no key), and minus delta.  Half precision, whose dp is scaled first: minus delta 2^-12.
-__device__ __forceinline__ float score_start(float lse, float c) { return lse == -INFINITY ? -INFINITY : -lse * kLog2e / c; }
+// What a row's scores and its dp start from: minus the logarithm of the row's sum (-infinity, every p zero, where the row has no key)
+// and minus delta.  With 16 bits the products of the scores begin at it, in units of the scores.  In float32 every step of a product
+// that carried it would round at its size, so it comes in behind them, s scale - lse rounded once and then taken to base 2: the error
+// is half a step of the exponent, which is small where p is large.
+// Half precision, whose dp is scaled first: minus delta 2^-12.
+template <typename T> constexpr bool kBehind = sizeof(T) == 4;
+template <typename T> __device__ __forceinline__ float score_factor(const Attn& a) {
+  return kBehind<T> ? (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) : exponent_factor(a);
+}
+template <typename T> __device__ __forceinline__ float score_start(float lse, float c) {
+  return lse == -INFINITY ? -INFINITY : kBehind<T> ? -lse : -lse * kLog2e / c;
+}
 // p and e, in the places of scores and dp that began so; shift: what is left to add to the exponents
-template <typename T> __device__ __forceinline__ void p_and_e(f32x4& s, f32x4& dp, float c, float shift, f32x4 minus_delta) {
+template <typename T> __device__ __forceinline__ void p_and_e(f32x4& s, f32x4& dp, float c, f32x4 shift, f32x4 minus_delta) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    s[r] = exp2_fast(fmaf(s[r], c, shift));
+    const float x = fmaf(s[r], c, shift[r]);
+    s[r] = exp2_fast(kBehind<T> ? x * kLog2e : x);
     dp[r] = s[r] * (kLift<T> > 0.f ? fmaf(dp[r], kLower<T>, minus_delta[r]) : dp[r]);
   }
 }
+template <typename T> __device__ __forceinline__ f32x4 s_start(f32x4 start) { return kBehind<T> ? all4(0.f) : start; }
+template <typename T> __device__ __forceinline__ f32x4 s_shift(f32x4 start) { return kBehind<T> ? start : all4(kLift<T>); }
 template <typename T> __device__ __forceinline__ f32x4 dp_start(f32x4 minus_delta) { return kLift<T> > 0.f ? all4(0.f) : minus_delta; }
 
 template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a, const Piece& b) {
@@ -144,7 +156,7 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 1
   if constexpr (KT * 16 < RK) {  // and e of them
     for (int x = lane; x < (RK - KT * 16) * LDE / E; x += 64) *reinterpret_cast<u32x4*>(ta + KT * 16 * LDE + x * E) = u32x4{0u, 0u, 0u, 0u};
   }
-  const float c = exponent_factor(a);
+  const float c = score_factor<T>(a);
   f32x4 dk[KT][DT], dv[KT][DT];
 #pragma unroll
   for (int t = 0; t < KT; ++t)
@@ -161,7 +173,7 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 1
 #pragma unroll
       for (int d = 1; d < PER; d *= 2) delta += __shfl_xor(delta, d);
       if (qp.c == 0 && qp.v[u] < CH) {
-        offs_all[qp.w[u]][qp.v[u]] = score_start(lse[u], c);
+        offs_all[qp.w[u]][qp.v[u]] = score_start<T>(lse[u], c);
         deltas_all[qp.w[u]][qp.v[u]] = delta * -kLower<T>;
       }
     }
@@ -187,13 +199,13 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 1
       }
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
-        f32x4 s = fo, dp = dp_start<T>(fd);
+        f32x4 s = s_start<T>(fo), dp = dp_start<T>(fd);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
           s = mma<T>(qf[f], kf[t][f], s);
           dp = mma<T>(gf[f], vf[t][f], dp);
         }
-        p_and_e<T>(s, dp, c, kLift<T>, fd);
+        p_and_e<T>(s, dp, c, s_shift<T>(fo), fd);
         const bool here = live >> t & 1;
         if (!__all(here)) {  // keys that no query looks at
 #pragma unroll
@@ -260,7 +272,7 @@ template <typename T, int DP, bool WHOLE> __global__ __launch_bounds__(256) void
   }
 #pragma unroll
   for (int d = PER / 2; d; d >>= 1) s += __shfl_xor(s, d);
-  if (x < all && threadIdx.x % PER == 0) a.stats[x] = make_float2(score_start(lse, exponent_factor(a)), s * -kLower<T>);
+  if (x < all && threadIdx.x % PER == 0) a.stats[x] = make_float2(score_start<T>(lse, score_factor<T>(a)), s * -kLower<T>);
 }
 
 // dk and dv: NW wavefronts of KW x 16 keys each hold keys, values and the sums of their gradients; the queries that look at them and
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
         *reinterpret_cast<u32x4*>(&gs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
       }
   }
-  const float c = exponent_factor(a);
+  const float c = score_factor<T>(a);
   if (a.scale < 0.f) {
 #pragma unroll
     for (int t = 0; t < KW; ++t)
@@ -385,7 +397,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
         const f32x4 o = *reinterpret_cast<const f32x4*>(offs[buf] + r + g4 * 4), l = *reinterpret_cast<const f32x4*>(deltas[buf] + r + g4 * 4);
 #pragma unroll
         for (int k = 0; k < KW; ++k) {
-          s[k][u] = o;
+          s[k][u] = s_start<T>(o);
           dp[k][u] = dp_start<T>(l);
         }
 #pragma unroll
@@ -398,7 +410,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
           }
         }
 #pragma unroll
-        for (int k = 0; k < KW; ++k) p_and_e<T>(s[k][u], dp[k][u], c, kLift<T>, l);
+        for (int k = 0; k < KW; ++k) p_and_e<T>(s[k][u], dp[k][u], c, s_shift<T>(o), l);
       }
       Piece p[KW][PQ], e[KW][PQ];
 #pragma unroll
@@ -481,7 +493,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   for (int u = 0; u < QT; ++u) {
     float2 st = make_float2(-INFINITY, 0.f);
     if (q[u].row >= 0) st = a.stats[stat_at(a, q[u].row, q[u].h)];
-    shift[u] = st.x * exponent_factor(a) + kLift<T>;
+    shift[u] = kBehind<T> ? st.x : st.x * exponent_factor(a) + kLift<T>;
     dp0[u] = all4(st.y);
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
@@ -498,7 +510,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
         *reinterpret_cast<u32x4*>(&vs[0][0] + x * LD + e) = u32x4{0u, 0u, 0u, 0u};
       }
   }
-  const float c = exponent_factor(a);
+  const float c = score_factor<T>(a);
   f32x4 dq[QT][DT];
 #pragma unroll
   for (int u = 0; u < QT; ++u)
@@ -536,7 +548,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
           }
         }
 #pragma unroll
-        for (int u = 0; u < QT; ++u) p_and_e<T>(s[u][x], dp[u][x], c, shift[u], dp0[u]);
+        for (int u = 0; u < QT; ++u) p_and_e<T>(s[u][x], dp[u][x], c, all4(shift[u]), dp0[u]);
       }
       Piece e[QT];
 #pragma unroll
