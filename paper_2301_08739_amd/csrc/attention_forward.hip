@@ -448,11 +448,10 @@ template <typename T, int DP, bool WHOLE> int run(const Attn& a, const Plan& p, 
   const Order order = make_order((int64_t)p.tg.tiles * a.K * p.splits);
   const uint32_t grid = workgroups(order);
   if (grid == 0) return FF_OK;
-  constexpr int BK = sizeof(T) == 2 && DP <= 32 ? 128 : 64;  // (fewer barriers: 16 elements 106 us instead of 117)
   if (p.rows == 16) {
     k_attention_tiles<T, DP, 1, 1, 32, WHOLE><<<grid, 64, 0, st>>>(a, p.tg, order, p.splits, ws);
   } else if (p.rows == 128) {
-    k_attention_tiles<T, DP, 4, 2, BK, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, order, p.splits, ws);
+    k_attention_tiles<T, DP, 4, 2, 64, WHOLE><<<grid, 256, 0, st>>>(a, p.tg, order, p.splits, ws);
   } else {
     if constexpr (sizeof(T) == 2 && DP == 128) k_attention_tiles<T, DP, 8, 2, 64, WHOLE><<<grid, 512, 0, st>>>(a, p.tg, order, p.splits, ws);
   }
