@@ -426,17 +426,23 @@ template <typename T, int DP, int HW, int CH> struct QueryPieces {
   typedef HeadRows<T, DP, HW, CH> H;
   int c;
   int32_t raw[H::U], row[H::U], h[H::U];
-  int v[H::U], w[H::U];  // v < 0: a row beyond the chunk's
-  // Chunk that begins at position p0; there: its positions
+  int v[H::U], w[H::U];  // v >= CH: none
+  // In the order in which rows and heads lie in memory.  Where `share` does not divide CH, every tile ends in rows that no position has;
+  // the pieces that are left clear them (their position is behind the chunk's end), as sums over a tile's rows run over them too.
   __device__ __forceinline__ void place(const Attn& a, int tid) {
     c = tid % H::PER;
+    const int used = quotient(CH, a.share) * a.share.by, over = CH - used;
 #pragma unroll
     for (int u = 0; u < H::U; ++u) {
       const int t = tid / H::PER + u * (H::NT / H::PER), s = quotient(t, a.share), p = s / HW;
       w[u] = s % HW;
       h[u] = w[u] * a.share.by + t - s * a.share.by;
       v[u] = p * a.share.by + t - s * a.share.by;
-      raw[u] = p;
+      if (t >= used * HW) {
+        const int left = t - used * HW;
+        w[u] = h[u] = left < over * HW ? left / over : 0;
+        v[u] = left < over * HW ? used + left % over : CH;
+      }
     }
   }
   __device__ __forceinline__ int position(const Attn& a, int u) const { return quotient(v[u], a.share); }

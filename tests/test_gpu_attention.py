@@ -137,6 +137,18 @@ def test_shared_heads(dtype, H, K):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,K", [(6, 2), (12, 4), (10, 2), (28, 4), (22, 2)])
+@pytest.mark.parametrize("D", [16, 32])
+def test_short_groups_after_calls_that_leave_nan_in_shared_memory(dtype, H, K, D):
+    """Heads that share a key by threes, fives and so on leave rows of a tile without a position: nothing of them may be summed."""
+    before = Case(dtype, [60] * 300, H=H, K=K, D=D, seed=1)
+    for x in (before.q, before.k, before.v, before.g):
+        x.fill_(float("nan"))
+    before.run()
+    Case(dtype, [40, 17, 60, 3] * 3, H=H, K=K, D=D, seed=H).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("lens", [([1], [1]), ([1], [4000]), ([3, 1], [0, 700]), ([0, 2], [5, 0]), ([200], [2500]), ([1, 1, 1, 1], [900, 1, 33, 3000]),
                                   ([2500], [3]), ([700, 20], [1, 90]), ([17], [129])], ids=str)
 @pytest.mark.parametrize("D", [16, 40, 128])
