@@ -259,7 +259,8 @@ int ff_group_attention_path(const ff_layer_weights* w, int G, int dtype, uint32_
  *
  * the last two summed also over the query heads that share a key head.  A query whose group holds no key, or none that the mask
  * leaves, gets out = 0, lse = -infinity and dq = 0, and a key without queries, or one that the mask takes out, dk = dv = 0.
- * What a masked row of k or v holds is of no account, infinities and NaNs included.
+ * What a masked row of k or v holds is of no account, infinities and NaNs included.  Keys whose score is -infinity count as keys
+ * that are not there, a row that has no other keys included; other infinities and NaNs go their way through the formulas.
  *
  * ff_heads: element e of head h of row r lies at data[r * row_stride + h * head_stride + e] (strides in elements, none
  * negative).  Inputs may have strides of zero; rows and heads of an output must not share elements with each other,
@@ -277,8 +278,9 @@ int ff_group_attention_path(const ff_layer_weights* w, int G, int dtype, uint32_
  * Results do not depend on timing: the same call gives the same bits.  16-bit types: products of that type with float32 sums;
  * scores, softmax, lse, delta and all sums are float32, and p and e are rounded to the type where they enter a product.
  * FF_F32: float32 throughout.
- * Limits (FF_ERR_UNSUPPORTED otherwise): head_dim 1..128, heads a multiple of kv_heads, rows < 2^31, strides below 4 GiB, and at most
- * 2^31 - 1 workgroups a launch (tiles of 16 rows and more, times heads). */
+ * Limits (FF_ERR_UNSUPPORTED otherwise): head_dim 1..128, heads a multiple of kv_heads, rows < 2^31 - 1024 of each list, for the
+ * gradient rows of queries * heads < 2^31, strides below 4 GiB, and at most 2^32 - 1 threads a launch (64 to 512 a tile of 16 to 256
+ * rows and key head, and 64 at least a group and key head). */
 typedef struct {
   void* data; /* read only where it is an input */
   int64_t row_stride, head_stride;
@@ -293,7 +295,7 @@ typedef struct {
 
 typedef struct {
   int32_t heads, kv_heads, head_dim;
-  float scale;                /* finite, usually 1 / sqrt(head_dim) */
+  float scale;                /* usually 1 / sqrt(head_dim); 1e30 at most, either sign */
   const int32_t* num_groups;  /* device scalar, or NULL */
   int32_t max_groups;
   ff_group_list queries, keys;
@@ -328,7 +330,8 @@ int ff_attention_backward(const ff_attention_shape* a, const ff_heads* q, const 
  * their precision; the result is rounded once.
  * q (q_heads heads of n rows) and k (k_heads, or 0 and k NULL) are turned in one launch; q_out may be q, and k_out may be k
  * (same address and strides); other overlaps are FF_ERR_ARG.
- * Limits (FF_ERR_UNSUPPORTED otherwise): axes 1..3, 1 <= axes * pairs <= 128, 2 * axes * pairs <= head_dim <= 256. */
+ * Limits (FF_ERR_UNSUPPORTED otherwise): axes 1..3, 1 <= axes * pairs <= 128, 2 * axes * pairs <= head_dim <= 256, 65536 heads, rows
+ * < 2^31, and below 2^24 workgroups of 16 KiB each (or of a row, where that is more). */
 typedef struct {
   int32_t axes, pairs; /* position columns, and turned pairs of each */
   int32_t layout;      /* FF_ROTARY_HALF | FF_ROTARY_INTERLEAVED */

@@ -102,22 +102,27 @@ Heads heads_of(const ff_heads* x, size_t size) { return {(char*)x->data, (uint32
 
 int check_list(const ff_group_list& l) {
   if (l.n < 0 || l.G < 1) return FF_ERR_ARG;
-  return l.n > INT32_MAX ? FF_ERR_UNSUPPORTED : FF_OK;
+  return l.n > INT32_MAX - 1024 ? FF_ERR_UNSUPPORTED : FF_OK;  // (a tile's last position is a number of 32 bits too)
 }
 int make_attention(const ff_attention_shape* a, int dtype, Attn* out) {
   if (!a || (dtype != FF_F32 && dtype != FF_BF16 && dtype != FF_F16)) return FF_ERR_ARG;
-  if (a->heads < 1 || a->kv_heads < 1 || a->head_dim < 1 || a->max_groups < 0 || !std::isfinite(a->scale)) return FF_ERR_ARG;
+  if (a->heads < 1 || a->kv_heads < 1 || a->head_dim < 1 || a->max_groups < 0 || !(std::fabs(a->scale) <= 1e30f)) return FF_ERR_ARG;
   if (a->heads % a->kv_heads || a->head_dim > 128) return FF_ERR_UNSUPPORTED;
   for (const ff_group_list* l : {&a->queries, &a->keys})
     if (const int st = check_list(*l); st != FF_OK) return st;
-  auto list = [](const ff_group_list& l) { return GroupList{l.perm, l.offsets, (int32_t)l.n, l.G < l.n ? l.G : (l.n ? (int32_t)l.n : 1)}; };
+  // (numbers of rows and masks of no rows hold nothing to read)
+  auto list = [&](const ff_group_list& l) {
+    const int32_t G = l.G < l.n ? l.G : (l.n ? (int32_t)l.n : 1);
+    const int64_t listed = (int64_t)a->max_groups * G;
+    return GroupList{l.n > 0 ? l.perm : nullptr, l.offsets, (int32_t)l.n, G, (int32_t)(listed < l.n ? listed : l.n)};
+  };
   *out = Attn{};
   out->H = a->heads; out->K = a->kv_heads; out->D = a->head_dim;
   out->share = make_div(a->heads / a->kv_heads);
   out->scale = a->scale;
   out->num_groups = a->num_groups; out->max_groups = a->max_groups;
   out->ql = list(a->queries); out->kl = list(a->keys);
-  out->mask = a->key_mask;
+  out->mask = a->keys.n > 0 ? a->key_mask : nullptr;
   return FF_OK;
 }
 int check_attention_call(const ff_attention_shape* a, const HeadsIn* arrays, int count, int dtype, const float* lse, bool lse_written,

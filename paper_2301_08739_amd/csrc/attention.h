@@ -12,6 +12,7 @@ struct GroupList {
   const int32_t* perm;  // or nullptr: position p is row p
   const int32_t* off;
   int32_t n, G;
+  int32_t slots;  // positions that groups can have: n, or the groups times G where that is less (few rows out of many)
 };
 struct Div {  // quotients of numbers below 2^31 by a constant: a multiplication instead of a division
   uint32_t by, mul, shift;
@@ -69,6 +70,8 @@ __device__ __forceinline__ Span span_of(const GroupList& l, int32_t g) {
   const int32_t from = clamp_to(l.off[g], l.n), to = clamp_to(l.off[g + 1], l.n), len = to - from;
   return {from, len < 0 ? 0 : len < l.G ? len : l.G};
 }
+// Where the sums of a group's first position lie in a workspace that has a place for every position of a list
+__device__ __forceinline__ int32_t slot_of(const GroupList& l, int32_t g, const Span& s) { return l.slots < l.n ? g * l.G : s.at; }
 // Row at position p, -1 where the list holds none of the rows.
 __device__ __forceinline__ int32_t row_at(const GroupList& l, int32_t p) {
   const int32_t r = l.perm ? l.perm[p] : p;

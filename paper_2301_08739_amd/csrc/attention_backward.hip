@@ -21,7 +21,7 @@ template <> constexpr float kLower<f16_t> = 1.f / 4096.f;
 // Half precision, whose dp is scaled first: minus delta 2^-12.
 template <typename T> constexpr bool kBehind = sizeof(T) == 4;
 template <typename T> __device__ __forceinline__ float score_factor(const Attn& a) {
-  return kBehind<T> ? (a.scale == 0.f ? 1e-30f : fabsf(a.scale)) : exponent_factor(a);
+  return kBehind<T> ? score_scale(a) : exponent_factor(a);
 }
 template <typename T> __device__ __forceinline__ float score_start(float lse, float c) {
   return lse == -INFINITY ? -INFINITY : kBehind<T> ? -lse : -lse * kLog2e / c;
@@ -438,8 +438,9 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 128 ? 2 : 1) void k_atte
     if (key[t] < 0) continue;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     if (splits > 1) {
-      const int64_t all = (int64_t)a.kl.n * a.K;
-      float* to = part + (split * all + (int64_t)key[t] * a.K + kh) * 2 * DP + g4 * 4;
+      const int32_t slot = slot_of(a.kl, at.g, sk) + k0 + (wave * KW + t) * 16 + i;
+      const int64_t all = (int64_t)a.kl.slots * a.K;
+      float* to = part + (split * all + (int64_t)slot * a.K + kh) * 2 * DP + g4 * 4;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         *reinterpret_cast<f32x4*>(to + d * 16) = live[t] ? dk[t][d] : zero;
@@ -565,8 +566,9 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= 256 ? 2 : 1) void k_atte
   for (int u = 0; u < QT; ++u) {
     if (q[u].row < 0) continue;
     if (splits > 1) {
-      const int64_t all = (int64_t)a.ql.n * a.H;
-      float* to = part + (split * all + stat_at(a, q[u].row, q[u].h)) * DP + g4 * 4;
+      const int32_t slot = slot_of(a.ql, at.g, sq) + quotient(at.tile * BQ + (wave * QT + u) * 16 + i, a.share);
+      const int64_t all = (int64_t)a.ql.slots * a.H;
+      float* to = part + (split * all + stat_at(a, slot, q[u].h)) * DP + g4 * 4;
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(to + d * 16) = dq[u][d];
       continue;
@@ -587,11 +589,12 @@ __global__ __launch_bounds__(256) void k_attention_sum(Attn a, GroupList l, Tile
   if (at.g < 0) return;
   const Span sp = span_of(l, at.g);
   if (at.tile > sp.len / ROWS) return;
-  const uint64_t all = (uint64_t)(uint32_t)l.n * heads * (N * DP);
+  const int32_t slot = slot_of(l, at.g, sp);
+  const uint64_t all = (uint64_t)(uint32_t)l.slots * heads * (N * DP);
   for (int r = tid / LANES; r < ROWS; r += 256 / LANES) {
     const int32_t p = at.tile * ROWS + r, row = p < sp.len ? row_at(l, sp.at + p) : -1;
     if (row < 0) continue;
-    const float* from = part + ((uint64_t)(uint32_t)row * heads + h) * (N * DP) + e;
+    const float* from = part + ((uint64_t)(uint32_t)(slot + p) * heads + h) * (N * DP) + e;
     f32x4 s = all4(0.f);
 #pragma unroll 4
     for (int k = 0; k < splits; ++k) s += *reinterpret_cast<const f32x4*>(from + k * all);
@@ -628,7 +631,7 @@ Plan plan(const Attn& a, size_t size) {
   if (!p.fits) return p;
   p.group = holds_group(DP, a.kl.G, size) && rows <= 512 && share <= 16;
   if (p.group) {
-    p.fits = (int64_t)a.max_groups * a.K <= INT32_MAX;
+    p.fits = one_launch((int64_t)a.max_groups * a.K, 64);
     return p;
   }
   bool f[4];
@@ -643,12 +646,14 @@ Plan plan(const Attn& a, size_t size) {
   const int64_t gq = (int64_t)p.tq.tiles * a.K, gk = (int64_t)p.tk.tiles * a.K;
   p.splits_q = stretches(p.tq, gq, p.rows == 16 ? 1 : 4, a.kl.G);
   p.splits_k = stretches(p.tk, gk, p.keys == 16 ? 1 : p.keys / 32, rows);
-  p.fits = f[0] && f[1] && gq * p.splits_q <= INT32_MAX - 128 && gk * p.splits_k <= INT32_MAX - 128 && (int64_t)a.ql.n * a.H <= INT32_MAX;
-  if (p.splits_q > 1) p.fits = p.fits && f[2] && (int64_t)p.sum_q.tiles * a.H <= INT32_MAX;
-  if (p.splits_k > 1) p.fits = p.fits && f[3] && (int64_t)p.sum_k.tiles * a.K <= INT32_MAX;
+  const int64_t stats = ceil_div((int64_t)a.ql.n * a.H * (DP * (int64_t)size / 16), 256);
+  p.fits = f[0] && f[1] && one_launch_in_order(gq * p.splits_q, p.rows == 16 ? 64 : 256) && (int64_t)a.ql.n * a.H <= INT32_MAX && one_launch(stats, 256) &&
+           one_launch_in_order(gk * p.splits_k, p.keys == 16 ? 64 : p.keys == 128 ? 256 : 512);
+  if (p.splits_q > 1) p.fits = p.fits && f[2] && one_launch((int64_t)p.sum_q.tiles * a.H, 256);
+  if (p.splits_k > 1) p.fits = p.fits && f[3] && one_launch((int64_t)p.sum_k.tiles * a.K, 256);
   p.stats = align_up((size_t)a.ql.n * a.H * 8, 256);
-  p.parts_q = p.splits_q > 1 ? align_up((size_t)p.splits_q * a.ql.n * a.H * DP * 4, 256) : 0;
-  p.parts_k = p.splits_k > 1 ? align_up((size_t)p.splits_k * a.kl.n * a.K * DP * 8, 256) : 0;
+  p.parts_q = p.splits_q > 1 ? align_up((size_t)p.splits_q * a.ql.slots * a.H * DP * 4, 256) : 0;
+  p.parts_k = p.splits_k > 1 ? align_up((size_t)p.splits_k * a.kl.slots * a.K * DP * 8, 256) : 0;
   p.bytes = p.stats + p.parts_q + p.parts_k;
   return p;
 }

@@ -298,9 +298,10 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
     if (q[u].row < 0) continue;
     const int64_t at_row = stat_at(a, q[u].row, q[u].h);
     if (splits > 1) {
-      const int64_t all = (int64_t)a.ql.n * a.H;
-      float* ml = part + (split * all + at_row) * 2;
-      float* po = part + splits * all * 2 + (split * all + at_row) * DP;
+      const int32_t slot = slot_of(a.ql, at.g, sq) + quotient(at.tile * BQ + (wave * QT + u) * 16 + i, a.share);
+      const int64_t all = (int64_t)a.ql.slots * a.H, at_slot = stat_at(a, slot, q[u].h);
+      float* ml = part + (split * all + at_slot) * 2;
+      float* po = part + splits * all * 2 + (split * all + at_slot) * DP;
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(po + d * 16 + g4 * 4) = o[u][d];
       if (g4 == 0) {
@@ -330,11 +331,13 @@ __global__ __launch_bounds__(256) void k_attention_join(Attn a, TileGrid tg, int
   const int kh = blockIdx.x / tg.tiles;
   const TileAt at = tile_at<1>(a, a.ql, tg, blockIdx.x - kh * tg.tiles, lane);
   if (at.g < 0) return;
-  const QueryRow q = query_row(a, span_of(a.ql, at.g), kh, at.tile);
+  const Span sq = span_of(a.ql, at.g);
+  const QueryRow q = query_row(a, sq, kh, at.tile);
   if (q.row < 0) return;
-  const int64_t all = (int64_t)a.ql.n * a.H, at_row = stat_at(a, q.row, q.h);
-  const float2* const ml = reinterpret_cast<const float2*>(part) + at_row;
-  const float* const po = part + splits * all * 2 + at_row * DP + tid % LANES * 4;
+  const int64_t all = (int64_t)a.ql.slots * a.H, at_row = stat_at(a, q.row, q.h);
+  const int64_t at_slot = stat_at(a, slot_of(a.ql, at.g, sq) + quotient(at.tile, a.share), q.h);
+  const float2* const ml = reinterpret_cast<const float2*>(part) + at_slot;
+  const float* const po = part + splits * all * 2 + at_slot * DP + tid % LANES * 4;
   constexpr int MINE = kMostSplits / 256;
   float2 mine[MINE];
   float top = kLowest;
@@ -395,7 +398,7 @@ Plan plan(const Attn& a, size_t size) {
     const int64_t waves = (int64_t)a.max_groups * a.K, tiles = ceil_div(rows, 16);
     const int64_t want = waves ? ceil_div(kChipWaves, waves) : 1;
     p.parts = (int)(want < tiles ? want : tiles);
-    p.fits = waves * p.parts <= INT32_MAX;
+    p.fits = one_launch(waves * p.parts, 64);
     return p;
   }
   // 128 rows (four wavefronts of 32) unless there are fewer than a third of that.  128 elements of 16 bits, two rounds of the chip and
@@ -415,12 +418,12 @@ Plan plan(const Attn& a, size_t size) {
   if (s > kMostSplits) s = kMostSplits;
   if (waves * 2 > kChipWaves) s = 1;
   p.splits = (int)s;
-  p.fits = p.fits && groups * s <= INT32_MAX - 128;
+  p.fits = p.fits && one_launch_in_order(groups * s, p.rows == 16 ? 64 : 2 * p.rows);
   if (s > 1) {
     bool fits;
     p.join = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, 1, &fits);
-    p.fits = p.fits && fits && (int64_t)p.join.tiles * a.K <= INT32_MAX;
-    p.bytes = (size_t)s * a.ql.n * a.H * (2 + DP) * 4;
+    p.fits = p.fits && fits && one_launch((int64_t)p.join.tiles * a.K, 256);
+    p.bytes = (size_t)s * a.ql.slots * a.H * (2 + DP) * 4;
   }
   return p;
 }

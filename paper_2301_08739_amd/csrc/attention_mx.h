@@ -190,8 +190,9 @@ __device__ __forceinline__ float over_lanes16_sum(float v) {
 }
 
 // Scores as they come from the products, as the exponents of p grow with them: c > 0, and the queries (or keys) negated where the
-// scale is negative; a scale of zero as next to nothing.
-__device__ __forceinline__ float exponent_factor(const Attn& a) { return a.scale == 0.f ? 1e-30f : fabsf(a.scale) * kLog2e; }
+// scale is negative; a scale of zero, or smaller than any score makes up for, as next to nothing.
+__device__ __forceinline__ float score_scale(const Attn& a) { return fmaxf(fabsf(a.scale), 1e-30f); }
+__device__ __forceinline__ float exponent_factor(const Attn& a) { return score_scale(a) * kLog2e; }
 
 // A launch's arguments lie in a few lines of memory that no cache holds yet; asked for one by one, as they are first used, each is a
 // trip.  So one word of every line is asked for at the start, all together.
@@ -251,6 +252,9 @@ inline Order make_order(int64_t total) {
   while (run > 1 && (total + 8 * run - 1) / (8 * run) * (8 * run) - total > total / 16) run /= 2;
   return {(uint32_t)total, run};
 }
+// A launch's threads are counted in 32 bits.
+inline bool one_launch(int64_t workgroups, int threads) { return workgroups <= (int64_t)(UINT32_MAX / threads); }
+inline bool one_launch_in_order(int64_t total, int threads) { return one_launch(total + total / 16 + 128, threads); }
 inline uint32_t workgroups(const Order& o) { return (o.total + 8 * o.run - 1) / (8 * o.run) * (8 * o.run); }
 
 // ---- a tile of rows into LDS ------------------------------------------------------------------------------

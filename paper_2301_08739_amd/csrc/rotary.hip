@@ -127,6 +127,7 @@ template <typename T, int V, int S, bool LOOSE = false> int launch(const Rotary&
   pl.rows = by_items < 1 ? 1 : by_items < by_angles ? by_items : by_angles;
   pl.row = make_div(pl.per_row);
   pl.head = make_div(per_head);
+  if (ceil_div(r.n, pl.rows) > (int64_t)(UINT32_MAX / 256)) return FF_ERR_UNSUPPORTED;  // (a launch's threads are counted in 32 bits)
   const dim3 grid((uint32_t)ceil_div(r.n, pl.rows), (uint32_t)ceil_div((int64_t)pl.rows * pl.per_row, kItems));
   k_rotary<T, V, S, LOOSE><<<grid, 256, 0, stream>>>(r, pl);
   return launch_status();

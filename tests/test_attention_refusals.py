@@ -62,6 +62,35 @@ def test_shapes(lib, bad, status):
     assert _backward(lib, s, ws=(AT["ws"], 1 << 40)) == status
 
 
+@pytest.mark.parametrize("bad,status", [(dict(scale=1.5e30), ARG), (dict(scale=-1.5e30), ARG), (dict(max_groups=1 << 28), UNSUPPORTED),
+                                        (dict(max_groups=1 << 28, head_dim=128), UNSUPPORTED),
+                                        (dict(queries=_GroupListC(None, AT["off"], (1 << 31) - 1, 32)), UNSUPPORTED),
+                                        (dict(keys=_GroupListC(None, AT["off"], (1 << 31) - 1, 32)), UNSUPPORTED)])
+def test_sizes_that_no_launch_counts(lib, bad, status):
+    s, x = _shape(**bad), _wide()
+    assert _forward(lib, s, **{n: x[n] for n in ("q", "k", "v", "out")}) == status
+    assert _backward(lib, s, ws=(AT["ws"], 1 << 40), **x) == status
+
+
+def _wide():                                           # heads of up to 128 elements
+    return {n: _HeadsC(i << 60, 512, 128) for i, n in enumerate(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), 1)}
+
+
+def test_rows_that_no_launch_counts(lib):
+    assert _backward(lib, _shape(nq=1 << 30, max_groups=1, head_dim=128, G=1 << 20), ws=(AT["ws"], 1 << 50), lse=9 << 60, **_wide()) == UNSUPPORTED
+    loose, out = (_HeadsC(1 << 60, 40000, 16) for _ in range(2))   # (in place: heads of 16 elements, 2,048 a row, turned one by one)
+    assert lib.ff_rotary(loose, out, 2048, None, None, 0, 1 << 25, 16, AT["pos"], 1, 1, _spec(pairs=7), 1, None) == UNSUPPORTED
+
+
+def test_workspaces_grow_with_the_rows_that_groups_can_have(lib):
+    sizes = []
+    for nq in (64, 1 << 24):
+        s = _shape(nq=nq, nk=1 << 20, G=4, key_G=1 << 20, max_groups=1)
+        sizes.append((lib.ff_attention_workspace_bytes(s, 1), lib.ff_attention_backward_workspace_bytes(s, 1)))
+    assert sizes[0][0] == sizes[1][0] > 0
+    assert sizes[1][1] - sizes[0][1] == ((1 << 24) - 64) * H * 8   # delta and the start of the scores, of every row
+
+
 def test_types_and_pointers(lib):
     s = _shape()
     assert _forward(lib, s, dtype=7) == ARG and _backward(lib, s, dtype=-1) == ARG

@@ -275,6 +275,94 @@ def test_same_bits_eagerly_on_a_stream_and_in_graphs(dtype, D, lens, lens_k):
     assert all(torch.equal(a, b) for a, b in zip(bufs, want))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,K", [(32, 1), (40, 2)])
+def test_many_heads_a_key(dtype, H, K):
+    Case(dtype, [20, 33, 1], H=H, K=K, D=16, seed=H).check()
+    Case(dtype, [1, 1], [90, 700], H=H, K=K, D=32, seed=H).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [16, 64])
+@pytest.mark.parametrize("G", [64, 500])
+def test_no_keys_at_all(dtype, D, G):
+    """A list and a mask of no rows, at addresses that hold something."""
+    c = Case(dtype, [3, 40], [0, 0], D=D, key_G=G, seed=21)
+    args, more = c.lists()
+    perm, mask = torch.zeros(4, dtype=torch.int32, device=DEV), torch.ones(4, dtype=torch.uint8, device=DEV)
+    more.update(key_perm=perm[:0], key_mask=mask[:0])
+    out, lse = torch.full_like(c.q, 5.0), torch.full((c.nq, c.H), 5.0, device=DEV)
+    dq, dk, dv = torch.full_like(c.q, 5.0), torch.empty_like(c.k), torch.empty_like(c.v)
+    ff.ff_attention(c.q, c.k, c.v, *args, out=out, lse=lse, **more)
+    ff.ff_attention_backward(c.q, c.k, c.v, out, lse, c.g, *args, dq=dq, dk=dk, dv=dv, **more)
+    assert (out == 0).all() and (lse == -torch.inf).all() and (dq == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [16, 64])
+def test_no_queries_at_all(dtype, D):
+    c = Case(dtype, [0, 0], [30, 200], D=D, seed=22)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,lens,lens_k", [("bf16", [3, 2], [3000, 900]), ("f32", [40, 1], [1, 2500]), ("f16", [300], [4000])])
+@pytest.mark.parametrize("D", [16, 128])
+def test_few_rows_out_of_many(dtype, lens, lens_k, D):
+    """Keys by stretches, whose sums have a place for each position that groups can have."""
+    c = Case(dtype, lens, lens_k, H=4, K=2, D=D, gap=3000, seed=23)
+    sizes = (c.H, c.K, D, c.nq, c.max_groups, c.G, {"f32": ff.FF_F32, "bf16": ff.FF_BF16, "f16": ff.FF_F16}[dtype], c.nk, c.key_G)
+    assert ff.ff_attention_workspace_bytes(*sizes) > 0
+    c.check()
+
+
+@pytest.mark.parametrize("lens", [[30, 40], [300, 20]], ids=str)
+def test_lists_left_out_and_masks_of_bools(lens):
+    """No numbers of rows: position p is row p.  No count: all listed groups.  A mask of bools is one of bytes."""
+    c = Case("bf16", lens, D=16, masked=0.3, shuffle=False, seed=24)
+    want = c.run()
+    args, more = c.lists()
+    out, lse = torch.zeros_like(c.q), torch.zeros_like(want[1])
+    grads = [torch.zeros_like(x) for x in (c.q, c.k, c.v)]
+    args = (None, args[1], None, c.max_groups, c.G)
+    more["key_mask"] = more["key_mask"].bool()
+    ff.ff_attention(c.q, c.k, c.v, *args, out=out, lse=lse, **more)
+    ff.ff_attention_backward(c.q, c.k, c.v, out, lse, c.g, *args, dq=grads[0], dk=grads[1], dv=grads[2], **more)
+    for a, b in zip((out, lse, *grads), want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("lens,lens_k", [([64] * 40, None), ([700, 900], None), ([2, 1], [3000, 5000])])
+def test_two_calls_at_once(lens, lens_k):
+    """On two streams, each with a workspace of its own."""
+    cases = [Case("bf16", lens, lens_k, H=4, K=2, D=32, seed=s) for s in (25, 26)]
+    want = [c.run() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                args, more = c.lists()
+                out, lse = torch.full_like(c.q, 5.0), torch.full((c.nq, c.H), 5.0, device=DEV)
+                grads = [torch.full_like(x, 5.0) for x in (c.q, c.k, c.v)]
+                ff.ff_attention(c.q, c.k, c.v, *args, out=out, lse=lse, **more)
+                ff.ff_attention_backward(c.q, c.k, c.v, out, lse, c.g, *args, dq=grads[0], dk=grads[1], dv=grads[2], **more)
+                got[i].append((out, lse, *grads))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,lens", [(16, [40, 64]), (64, [300])])
+@pytest.mark.parametrize("scale", [1e-38, -1e-33, 1e-42])
+def test_scales_next_to_nothing(dtype, D, lens, scale):
+    c = Case(dtype, lens, D=D, seed=27)
+    c.scale = scale
+    c.check()
+
+
 @pytest.mark.parametrize("D", [16, 64])
 def test_broadcast_keys_and_their_gradient(D):
     """One key and value head, spread over all heads by strides of zero; the gradient goes to heads of its own."""
