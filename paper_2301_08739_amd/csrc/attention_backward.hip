@@ -61,8 +61,12 @@ template <typename T> __device__ __forceinline__ float dot_pieces(const Piece& a
 // (dv)^T = dout^T p and (dk)^T = q^T e as they lie in the registers.  For (dq)^T = K^T e^T e goes through LDS once, which turns it.
 // All rows come and go through LDS, for the workgroup's heads together.  Region A: keys, then e, then dk; B: values, then queries (and dq
 // in their places) and dout by CH rows, then dv.  delta is summed where the rows of dout and out come in.
+// Registers decide how many wavefronts a SIMD takes: three for 64 keys of 16 elements (30,000 rows of 8 heads: 21.4 us, with two 23.5, with
+// four and some registers in scratch memory 30.7), two as long as that leaves next to none in scratch memory (80 keys in three: 30.1 for 29.7,
+// 96 keys: 43 for 32), else one.
 template <typename T, int DP, int KT, int HW, bool WHOLE>
-__global__ __launch_bounds__(64 * HW, KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 128 : 96) : 192) ? 2 : 1) void k_attention_backward_group(Attn a, Items items) {
+__global__ __launch_bounds__(64 * HW, KT * DP <= 64 && DP * sizeof(T) <= 64 ? 3 : KT * DP <= (sizeof(T) == 4 ? (DP == 16 ? 128 : 96) : 192) ? 2 : 1)
+void k_attention_backward_group(Attn a, Items items) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * HW;
   constexpr int CH = DP * (int)sizeof(T) <= 32 ? 32 : 16;  // (one piece of each array a thread, two of rows of 128 bytes)
   constexpr int KP = (KT + TILES - 1) / TILES, RK = KP * TILES * 16, PAD = 16 / (int)sizeof(T), LD = DP + PAD, LDE = 16 + PAD;
@@ -636,9 +640,11 @@ Plan plan(const Attn& a, size_t size) {
   }
   bool f[4];
   // Few rows go to one wavefront.  Long lists of 16-bit keys of 64 and more elements go by 256 to eight wavefronts, which share what they
-  // read (4,096 keys of 64 elements: 304 us instead of 336, of 128: 650 instead of 720; of groups of 64 keys: 217 instead of 130).
+  // read (4,096 keys of 64 elements: 304 us instead of 336, of 128: 650 instead of 720; of groups of 64 keys: 217 instead of 130),
+  // unless groups are uneven, where smaller tiles fill the chip better (30 of 1 to 4,000 keys of 64 elements: 1053 us instead of 1009).
   p.rows = rows > 32 ? 128 : 16;
-  p.keys = a.kl.G <= 32 ? 16 : size == 2 && DP >= 64 && a.kl.G >= 1024 ? 256 : 128;
+  const bool even = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, 256, &f[1]).per_group.by != 0;
+  p.keys = a.kl.G <= 32 ? 16 : size == 2 && DP >= 64 && a.kl.G >= 1024 && even ? 256 : 128;
   p.tq = tile_grid(a.ql.n, a.ql.G, share, a.max_groups, p.rows, &f[0]);
   p.tk = tile_grid(a.kl.n, a.kl.G, 1, a.max_groups, p.keys, &f[1]);
   p.sum_q = tile_grid(a.ql.n, a.ql.G, 1, a.max_groups, 64, &f[2]);
