@@ -10,6 +10,10 @@ namespace {
 // Keys and values come through LDS into registers once (values turned there), the queries by CH rows, of which a wavefront takes 16 at
 // a time; results go back the way the queries came.  Region A holds keys, then queries, then results; B values.  Of 32 elements and
 // more B is A: two more barriers, and twice the wavefronts a compute unit has LDS for.
+//
+// Large launches are near the memory's rate (240,000 rows, groups of 69, 8 heads of 32 elements of 16 bits: 118 us, 4.2 TB/s; groups of 64,
+// 16 elements: 58 us, 4.2 TB/s), small ones a chain of three trips (lists, rows, results; 30,000 rows: 12 us), float32 the matrix unit
+// (80,000 rows, groups of 128, 16 elements: 72 us, 73 TFLOP/s, the unit 51 % busy).
 template <typename T, int DP, int KT, int HW, bool WHOLE>
 __global__ __launch_bounds__(64 * HW, KT * DP <= 256 ? 2 : 1) void k_attention_group(Attn a, Items items) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * HW;
@@ -165,7 +169,10 @@ __global__ __launch_bounds__(64 * HW, KT * DP <= 256 ? 2 : 1) void k_attention_g
 // score.  Products start from minus infinity instead of zero for keys that are not there.  The running maximum may be too low by a
 // factor of 2^8 in p (no type's range minds), so that lanes need not compare notes: only where a lane finds a score beyond that, or its
 // row has met no key yet, is the maximum made good and what was summed brought down.  The sum of p is one of float32 additions: a
-// product with ones would sum the rounded p, and lse would be 2^-9 off.
+// product with ones would sum the rounded p, and lse would be 2^-9 off.  4 groups of 4,096 rows, 8 heads, bfloat16: 960 TFLOP/s of 128
+// elements, 710 of 64, 500 of 32; 12 groups of 1 to 6,000 rows of 64: 300 us, vector unit 70 % busy, matrix unit 35 %.  One wavefront to a
+// workgroup (32 rows and fewer) reads keys and values at 4.8 TB/s (one row, 32 heads on 8 of 65,537 keys, 128 elements: 56 us, join 6.5).
+// A wavefront without rows, in a group's last tile, only loads (200 rows: 46.4 us instead of 47.3).
 template <typename T, int DP, int NW, int QT, int BK, bool WHOLE>
 __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) || (DP == 64 && NW == 4) ? 2 : 1) void k_attention_tiles(Attn a, TileGrid tg, Order order, int splits, float* part) {
   constexpr int KF = Mx<T>::KF, E = Mx<T>::E, TILES = Mx<T>::TILES, NF = (DP + KF - 1) / KF, DT = DP / 16, NT = 64 * NW;
@@ -186,6 +193,8 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
   if ((int64_t)at.tile * BQ >= (int64_t)sq.len * tg.share) return;
   const int32_t tiles = (sk.len + BK - 1) / BK, per = (tiles + splits - 1) / splits;
   const int32_t t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
+
+  const bool busy = NW == 1 || at.tile * BQ + __builtin_amdgcn_readfirstlane(wave) * (QT * 16) < sq.len * tg.share;  // has this wavefront rows?
 
   KeyTiles<T, DP, BK, NT> kt;
   kt.next(a, sk, t0, t1, tid);
@@ -289,7 +298,7 @@ __global__ __launch_bounds__(64 * NW, DP * sizeof(T) <= (NW == 1 ? 256 : 128) ||
       kt.template fetch<WHOLE>(a, sk, t + 1, kh, tid);
       kt.next(a, sk, t + 2, t1, tid);
     }
-    tile(ks[buf], vs[buf], bias[buf]);
+    if (busy) tile(ks[buf], vs[buf], bias[buf]);
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
